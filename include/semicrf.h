@@ -409,6 +409,95 @@ int semicrf_scan_report(const void *workspace, size_t workspace_bytes, int B, in
 int semicrf_seq_report(const void *workspace, size_t workspace_bytes, int B, int T, int K, int C,
                        int ckpt_interval, int want_grad, int32_t *range_exceeded, double *logz64, void *stream);
 
+/*
+ * Encoder operators: what stands between tokens and the emission scores of the calls above.
+ *
+ * Activations (embeddings, u, x, b, c, dt, y and their gradients) are float, or 2-byte elements with SEMICRF_EMIS_F16 /
+ * SEMICRF_EMIS_BF16 in `flags`, all of one call alike; parameters, their gradients and states are float.  Sums, states and
+ * statistics are held in 32 bits or more whatever the type.  `lengths` is as everywhere (NULL = all T): rows t >= lengths[b]
+ * of an input are never read, those of an output are written as 0.  A `_row` argument is the distance, in elements, of one
+ * token's row from the next; sequence b begins B-major at row b*T.  So x, b and c may be columns of one array (the
+ * convolution's output), and gradients may be written side by side into one.  Rows that are read or written 16 bytes
+ * at a time (all but dt and grad_dt) begin on 16-byte boundaries (SEMICRF_EINVAL otherwise).  Results do not depend on
+ * timing: there are no floating-point atomics.  A value that is not finite in a valid row may spread over that sequence's
+ * results (and over the sums over sequences), earlier positions of the same 32 included; other sequences are not touched.
+ */
+
+/* flags bit 11 (semicrf_conv_fwd, semicrf_conv_bwd, semicrf_ssm_step): no SiLU after the convolution. */
+#define SEMICRF_CONV_LINEAR 2048u
+
+/*
+ * Token embedding: out[b,t,:] = scale * table[tokens[b,t],:].
+ *   tokens [B,T] int32; a token outside [0,V) has a row of zeros and no gradient (padding, masked positions)
+ *   table  [V,D], out [B,T,D] activations; D a multiple of 8, V <= 2^24
+ * semicrf_embed_bwd: grad_table[v,:] = scale * sum of grad_out[b,t,:] over the valid positions that hold v, float [V,D], fully
+ * overwritten; positions are sorted by token and added up in that order, so equal calls give equal bits.
+ */
+int semicrf_embed_fwd(const int32_t *tokens, const int32_t *lengths, const void *table, float scale, int B, int T, int V,
+                      int D, unsigned flags, void *out, void *stream);
+int semicrf_embed_bwd_workspace_bytes(int B, int T, int V, int D, size_t *bytes);
+int semicrf_embed_bwd(const int32_t *tokens, const int32_t *lengths, const void *grad_out, float scale, int B, int T, int V,
+                      int D, unsigned flags, void *workspace, size_t workspace_bytes, float *grad_table, void *stream);
+
+/*
+ * Short causal convolution, one filter of width W (1..4) per channel, followed by SiLU:
+ *     a[b,t,c] = bias[c] + sum_j weight[c,j] u[b,t-W+1+j,c]        out = a * sigmoid(a)
+ *   u, out [B,T,C] activations, C a multiple of 8; weight [C,W], bias [C] (or NULL) float
+ *   ring   [B,C,W] activations or NULL, seen [B] int32 (or NULL without ring): the call continues sequences of which
+ *          seen[b] tokens have gone before; ring[b,c,p mod W] holds u at position p for the last W of them.  NULL: zeros.
+ *          seen[b] < 0 marks a slot without a sequence: its output is 0 and its ring stays.
+ *   ring_out [B,C,W] or NULL: the ring after the call's tokens; may be `ring` itself.
+ * semicrf_conv_bwd (sequences from their beginning): grad_u like u, grad_weight [C,W], grad_bias [C] or NULL, fully
+ * overwritten.
+ */
+int semicrf_conv_fwd(const void *u, int64_t u_row, const float *weight, const float *bias, const int32_t *lengths,
+                     const int32_t *seen, const void *ring, int B, int T, int C, int W, unsigned flags, void *out,
+                     int64_t out_row, void *ring_out, void *stream);
+int semicrf_conv_bwd_workspace_bytes(int B, int T, int C, int W, size_t *bytes);
+int semicrf_conv_bwd(const void *u, int64_t u_row, const float *weight, const float *bias, const int32_t *lengths,
+                     const void *grad_out, int64_t grad_out_row, int B, int T, int C, int W, unsigned flags,
+                     void *workspace, size_t workspace_bytes, void *grad_u, int64_t grad_u_row, float *grad_weight,
+                     float *grad_bias, void *stream);
+
+/*
+ * Selective state space scan.  For each head h of H (P channels, a P x N state) with delta = softplus(dt + dt_bias):
+ *     H_t = exp(delta_t rate) H_{t-1} + delta_t x_t B_t^T          y_t = H_t C_t + skip x_t
+ *   x, y [B,T,H*P], b, c [B,T,G*N], dt [B,T,H] activations; each of G groups of H/G heads shares B_t and C_t
+ *   rate, skip (or NULL: 0), dt_bias (or NULL: 0) [H] float; rate < 0 is what forgets
+ *   state, state_out [B,H,P,N] float or NULL: the state before the first and after the last valid token (NULL: zeros / not
+ *          wanted); may be the same array, so a prompt can be taken in pieces
+ * P and N are multiples of 8 up to 128.  Workspace: semicrf_ssm_workspace_bytes, want_grad = 0 for semicrf_ssm_fwd (may be 0
+ * bytes), 1 for semicrf_ssm_bwd.
+ * semicrf_ssm_bwd takes the same inputs, grad_y like y, and grad_state_out [B,H,P,N] or NULL (zeros); it writes grad_x,
+ * grad_b, grad_c, grad_dt like x, b, c, dt, grad_rate [H], and where they are not NULL grad_skip [H], grad_dt_bias [H] and
+ * grad_state [B,H,P,N] (the gradient of `state`).
+ */
+int semicrf_ssm_workspace_bytes(int B, int T, int H, int P, int G, int N, int want_grad, size_t *bytes);
+int semicrf_ssm_fwd(const void *x, int64_t x_row, const void *b, int64_t b_row, const void *c, int64_t c_row,
+                    const void *dt, int64_t dt_row, const float *rate, const float *skip, const float *dt_bias,
+                    const int32_t *lengths, const float *state, int B, int T, int H, int P, int G, int N,
+                    unsigned flags, void *workspace, size_t workspace_bytes, void *y, int64_t y_row,
+                    float *state_out, void *stream);
+int semicrf_ssm_bwd(const void *x, int64_t x_row, const void *b, int64_t b_row, const void *c, int64_t c_row,
+                    const void *dt, int64_t dt_row, const float *rate, const float *skip, const float *dt_bias,
+                    const int32_t *lengths, const float *state, const void *grad_y, int64_t grad_y_row,
+                    const float *grad_state_out, int B, int T, int H, int P, int G, int N, unsigned flags,
+                    void *workspace, size_t workspace_bytes, void *grad_x, int64_t grad_x_row, void *grad_b,
+                    int64_t grad_b_row, void *grad_c, int64_t grad_c_row, void *grad_dt, int64_t grad_dt_row,
+                    float *grad_rate, float *grad_skip, float *grad_dt_bias, float *grad_state, void *stream);
+
+/*
+ * One more token of each of B streams: the convolution over C = H*P + 2*G*N channels (x, then B, then C, as they stand side by
+ * side in `u` [B,C], rows of any alignment) and one step of the scan, in one launch and without a workspace.
+ *   seen [B] int32: tokens before this one (the ring's convention above); < 0 marks an idle slot: y = 0, ring and state stay
+ *   ring, ring_out [B,C,W], state, state_out [B,H,P,N]: each pair may be the same array
+ *   dt [B,H], y [B,H*P]; everything else as above.  What the convolution gives stays in 32 bits here.
+ */
+int semicrf_ssm_step(const void *u, int64_t u_row, const float *weight, const float *bias, const void *dt, int64_t dt_row,
+                     const float *rate, const float *skip, const float *dt_bias, const int32_t *seen, const void *ring,
+                     const float *state, int B, int H, int P, int G, int N, int W, unsigned flags, void *y,
+                     void *ring_out, float *state_out, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

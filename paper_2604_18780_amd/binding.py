@@ -21,7 +21,10 @@ EXPORTS = ("semicrf_version", "semicrf_strerror", "semicrf_workspace_bytes",
            "semicrf_fwd_bwd_boundary", "semicrf_entropies", "semicrf_viterbi_workspace_bytes",
            "semicrf_viterbi", "semicrf_durtrans_workspace_bytes", "semicrf_durtrans_ckpt_interval", "semicrf_logz_fwd_durtrans",
            "semicrf_fwd_bwd_durtrans", "semicrf_fwd_bwd_static", "semicrf_seq_report",
-           "semicrf_ckpt_interval_low_memory", "semicrf_entropies_workspace_bytes", "semicrf_entropies_ws")
+           "semicrf_ckpt_interval_low_memory", "semicrf_entropies_workspace_bytes", "semicrf_entropies_ws",
+           "semicrf_embed_fwd", "semicrf_embed_bwd_workspace_bytes", "semicrf_embed_bwd", "semicrf_conv_fwd",
+           "semicrf_conv_bwd_workspace_bytes", "semicrf_conv_bwd", "semicrf_ssm_workspace_bytes", "semicrf_ssm_fwd",
+           "semicrf_ssm_bwd", "semicrf_ssm_step")
 SEMICRF_STATIC_WORKSPACE_BYTES = 64 << 20
 SEMICRF_CENTER = 1
 SEMICRF_SEQUENTIAL_SCAN = 2
@@ -34,6 +37,7 @@ SEMICRF_VITERBI_GLOBAL_TRACE = 128
 SEMICRF_LOW_MEMORY = 256
 SEMICRF_TWO_WAVE_SCAN = 512
 SEMICRF_ONE_WAVE_SCAN = 1024
+SEMICRF_CONV_LINEAR = 2048
 PLAN_LOW_MEMORY = 8   # added to want_grad for the workspace of SEMICRF_LOW_MEMORY calls
 
 
@@ -119,6 +123,21 @@ def load():
     lib.semicrf_seq_report.argtypes = [vp, sz, ci, ci, ci, ci, ci, ci, vp, vp, vp]
     lib.semicrf_ckpt_interval_low_memory.restype = ci
     lib.semicrf_ckpt_interval_low_memory.argtypes = [ci, ci, ci, ci, ci, ctypes.POINTER(ci)]
+    cf, cl, psz = ctypes.c_float, ctypes.c_int64, ctypes.POINTER(sz)
+    for name, args in {
+        "semicrf_embed_fwd": [vp, vp, vp, cf, ci, ci, ci, ci, cu, vp, vp],
+        "semicrf_embed_bwd_workspace_bytes": [ci, ci, ci, ci, psz],
+        "semicrf_embed_bwd": [vp, vp, vp, cf, ci, ci, ci, ci, cu, vp, sz, vp, vp],
+        "semicrf_conv_fwd": [vp, cl, vp, vp, vp, vp, vp, ci, ci, ci, ci, cu, vp, cl, vp, vp],
+        "semicrf_conv_bwd_workspace_bytes": [ci, ci, ci, ci, psz],
+        "semicrf_conv_bwd": [vp, cl, vp, vp, vp, vp, cl, ci, ci, ci, ci, cu, vp, sz, vp, cl, vp, vp, vp],
+        "semicrf_ssm_workspace_bytes": [ci] * 7 + [psz],
+        "semicrf_ssm_fwd": [vp, cl] * 4 + [vp] * 5 + [ci] * 6 + [cu, vp, sz, vp, cl, vp, vp],
+        "semicrf_ssm_bwd": [vp, cl] * 4 + [vp] * 5 + [vp, cl, vp] + [ci] * 6 + [cu, vp, sz] + [vp, cl] * 4 + [vp] * 5,
+        "semicrf_ssm_step": [vp, cl, vp, vp, vp, cl] + [vp] * 6 + [ci] * 6 + [cu] + [vp] * 4,
+    }.items():
+        getattr(lib, name).restype = ci
+        getattr(lib, name).argtypes = args
     _lib = lib
     return lib
 
@@ -496,3 +515,182 @@ def semicrf_fwd_bwd_profiled(emis, lengths, trans, dur, events, grad_logz=None, 
         _ptr(g_e, torch.float32), _ptr(g_t, torch.float32), _ptr(g_d, torch.float32),
         _ptr(pm, torch.float32), _stream(), events.arr))
     return out
+
+
+# ---- encoder operators ----------------------------------------------------------------------------------------------
+
+_ACT = {torch.float32: 0, torch.float16: SEMICRF_EMIS_F16, torch.bfloat16: SEMICRF_EMIS_BF16}
+
+
+def _act(t) -> int:
+    """The flags bits of a tensor's storage type."""
+    if t.dtype not in _ACT:
+        raise ValueError("activations must be float32, float16 or bfloat16")
+    return _ACT[t.dtype]
+
+
+def _rows(t, dtype, shape):
+    """Pointer and row distance of activations [B,T,...] (or [B,...]) whose trailing dimensions lie side by side."""
+    if t is None or not t.is_cuda or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"expected a {dtype} device tensor of shape {tuple(shape)}")
+    width, lead = 1, 2 if len(shape) > 2 else 1
+    for d in range(len(shape) - 1, lead - 1, -1):
+        if shape[d] != 1 and t.stride(d) != width:
+            raise ValueError("the trailing dimensions of a row must lie side by side")
+        width *= shape[d]
+    row = t.stride(lead - 1) if shape[lead - 1] > 1 else (t.stride(0) if lead == 2 and shape[0] > 1 else width)
+    if lead == 2 and shape[0] > 1 and t.stride(0) != shape[1] * row:
+        raise ValueError("rows of successive sequences must follow each other")
+    return t.data_ptr(), row
+
+
+def _param(t, shape):
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"expected a parameter of shape {tuple(shape)}")
+    return _ptr(t, torch.float32)
+
+
+def _index(t, shape):
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"expected an int32 tensor of shape {tuple(shape)}")
+    return _ptr(t, torch.int32)
+
+
+def _plain(t, dtype, shape):
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"expected a tensor of shape {tuple(shape)}")
+    return _ptr(t, dtype)
+
+
+def _scratch(entry, sizes, device):
+    """A workspace of the size the library asks for (torch aligns it to 512 bytes)."""
+    n = ctypes.c_size_t(0)
+    _check(getattr(load(), entry)(*sizes, ctypes.byref(n)))
+    return torch.empty(n.value, dtype=torch.uint8, device=device)
+
+
+def semicrf_embed_fwd(tokens, table, scale=1.0, lengths=None, out=None):
+    """scale * table[tokens] as [B,T,D] in the table's type; tokens outside the table and positions beyond `lengths` are 0."""
+    B, T = tokens.shape
+    V, D = table.shape
+    if out is None:
+        out = torch.empty((B, T, D), dtype=table.dtype, device=table.device)
+    _check(load().semicrf_embed_fwd(_index(tokens, (B, T)), _index(lengths, (B,)), _ptr(table, table.dtype), scale, B, T, V,
+                                    D, _act(table), _plain(out, table.dtype, (B, T, D)), _stream()))
+    return out
+
+
+def semicrf_embed_bwd(tokens, grad_out, V, scale=1.0, lengths=None, workspace=None, grad_table=None):
+    """The gradient [V,D] (float32) of semicrf_embed_fwd's table."""
+    B, T = tokens.shape
+    D = grad_out.shape[-1]
+    if workspace is None:
+        workspace = _scratch("semicrf_embed_bwd_workspace_bytes", (B, T, V, D), grad_out.device)
+    if grad_table is None:
+        grad_table = torch.empty((V, D), dtype=torch.float32, device=grad_out.device)
+    _check(load().semicrf_embed_bwd(_index(tokens, (B, T)), _index(lengths, (B,)),
+                                    _plain(grad_out, grad_out.dtype, (B, T, D)), scale, B, T, V, D, _act(grad_out),
+                                    workspace.data_ptr(), workspace.numel(), _plain(grad_table, torch.float32, (V, D)),
+                                    _stream()))
+    return grad_table
+
+
+def semicrf_conv_fwd(u, weight, bias=None, lengths=None, ring=None, seen=None, flags=0, ring_out=None, out=None):
+    """Causal convolution and SiLU of u [B,T,C] with weight [C,W]; a given `ring` [B,C,W] with `seen` [B] continues sequences,
+    and `ring_out` (which may be `ring`) receives the ring after this call's tokens."""
+    B, T, C = u.shape
+    W = weight.shape[1]
+    if out is None:
+        out = torch.empty((B, T, C), dtype=u.dtype, device=u.device)
+    _check(load().semicrf_conv_fwd(*_rows(u, u.dtype, (B, T, C)), _param(weight, (C, W)), _param(bias, (C,)),
+                                   _index(lengths, (B,)), _index(seen, (B,)), _plain(ring, u.dtype, (B, C, W)), B, T, C, W,
+                                   flags | _act(u), *_rows(out, u.dtype, (B, T, C)),
+                                   _plain(ring_out, u.dtype, (B, C, W)), _stream()))
+    return out
+
+
+def semicrf_conv_bwd(u, weight, bias, grad_out, lengths=None, flags=0, workspace=None, grad_u=None):
+    """Returns (grad_u like u, grad_weight [C,W], grad_bias [C]) of semicrf_conv_fwd without a ring."""
+    B, T, C = u.shape
+    W = weight.shape[1]
+    dev = u.device
+    if workspace is None:
+        workspace = _scratch("semicrf_conv_bwd_workspace_bytes", (B, T, C, W), dev)
+    if grad_u is None:
+        grad_u = torch.empty((B, T, C), dtype=u.dtype, device=dev)
+    gw = torch.empty((C, W), dtype=torch.float32, device=dev)
+    gb = torch.empty(C, dtype=torch.float32, device=dev)
+    _check(load().semicrf_conv_bwd(*_rows(u, u.dtype, (B, T, C)), _param(weight, (C, W)), _param(bias, (C,)),
+                                   _index(lengths, (B,)), *_rows(grad_out, u.dtype, (B, T, C)), B, T, C, W,
+                                   flags | _act(u), workspace.data_ptr(), workspace.numel(),
+                                   *_rows(grad_u, u.dtype, (B, T, C)), gw.data_ptr(), gb.data_ptr(), _stream()))
+    return grad_u, gw, gb
+
+
+def _ssm_inputs(x, b, c, dt, rate, skip, dt_bias, lengths, state):
+    B, T, H, P = x.shape
+    G, N = b.shape[2:]
+    return (B, T, H, P, G, N), (*_rows(x, x.dtype, (B, T, H, P)), *_rows(b, x.dtype, (B, T, G, N)),
+                                *_rows(c, x.dtype, (B, T, G, N)), *_rows(dt, x.dtype, (B, T, H)), _param(rate, (H,)),
+                                _param(skip, (H,)), _param(dt_bias, (H,)), _index(lengths, (B,)),
+                                _param(state, (B, H, P, N)))
+
+
+def semicrf_ssm_fwd(x, b, c, dt, rate, skip=None, dt_bias=None, lengths=None, state=None, want_state=True,
+                    workspace=None, out=None, state_out=None):
+    """Selective state space scan of x [B,T,H,P] with b, c [B,T,G,N] and dt [B,T,H], from `state` [B,H,P,N] (None: zeros).
+    Returns (y [B,T,H,P], state after the last token or None)."""
+    sizes, inputs = _ssm_inputs(x, b, c, dt, rate, skip, dt_bias, lengths, state)
+    B, T, H, P, G, N = sizes
+    if workspace is None:
+        workspace = _scratch("semicrf_ssm_workspace_bytes", (*sizes, 0), x.device)
+    if out is None:
+        out = torch.empty((B, T, H, P), dtype=x.dtype, device=x.device)
+    if state_out is None and want_state:
+        state_out = torch.empty((B, H, P, N), dtype=torch.float32, device=x.device)
+    _check(load().semicrf_ssm_fwd(*inputs, *sizes, _act(x), workspace.data_ptr(), workspace.numel(),
+                                  *_rows(out, x.dtype, (B, T, H, P)), _param(state_out, (B, H, P, N)), _stream()))
+    return out, state_out
+
+
+def semicrf_ssm_bwd(x, b, c, dt, rate, skip, dt_bias, grad_y, lengths=None, state=None, grad_state_out=None,
+                    want_state=False, workspace=None):
+    """Gradients of semicrf_ssm_fwd as a dict: grad_xbc [B,T,H*P+2*G*N] (those of x, b and c side by side, also as views grad_x,
+    grad_b, grad_c), grad_dt, grad_rate, grad_skip, grad_dt_bias and, with want_state, grad_state."""
+    sizes, inputs = _ssm_inputs(x, b, c, dt, rate, skip, dt_bias, lengths, state)
+    B, T, H, P, G, N = sizes
+    dev, dtype, f32 = x.device, x.dtype, torch.float32
+    if workspace is None:
+        workspace = _scratch("semicrf_ssm_workspace_bytes", (*sizes, 1), dev)
+    gxbc = torch.empty((B, T, H * P + 2 * G * N), dtype=dtype, device=dev)
+    gx = gxbc[..., :H * P].unflatten(2, (H, P))
+    gb = gxbc[..., H * P:H * P + G * N].unflatten(2, (G, N))
+    gc = gxbc[..., H * P + G * N:].unflatten(2, (G, N))
+    gdt = torch.empty((B, T, H), dtype=dtype, device=dev)
+    heads = torch.empty((3, H), dtype=f32, device=dev)
+    gstate = torch.empty((B, H, P, N), dtype=f32, device=dev) if want_state else None
+    _check(load().semicrf_ssm_bwd(*inputs, *_rows(grad_y, dtype, (B, T, H, P)), _param(grad_state_out, (B, H, P, N)), *sizes,
+                                  _act(x), workspace.data_ptr(), workspace.numel(), *_rows(gx, dtype, (B, T, H, P)),
+                                  *_rows(gb, dtype, (B, T, G, N)), *_rows(gc, dtype, (B, T, G, N)),
+                                  *_rows(gdt, dtype, (B, T, H)), heads[0].data_ptr(), heads[1].data_ptr(),
+                                  heads[2].data_ptr(), _param(gstate, (B, H, P, N)), _stream()))
+    return dict(grad_xbc=gxbc, grad_x=gx, grad_b=gb, grad_c=gc, grad_dt=gdt, grad_rate=heads[0], grad_skip=heads[1],
+                grad_dt_bias=heads[2], grad_state=gstate)
+
+
+def semicrf_ssm_step(u, weight, bias, dt, rate, skip, dt_bias, seen, ring, state, groups=1, flags=0, out=None):
+    """One more token of each stream: u [B,H*P+2*G*N] (x, B and C before the convolution), ring [B,C,W], state [B,H,P,N], both
+    updated in place unless `out` = (y, ring_out, state_out) names other arrays.  Returns y [B,H*P]."""
+    B, H, P, N = state.shape
+    G, W = groups, weight.shape[1]
+    C = H * P + 2 * G * N
+    if out is None:
+        out = (torch.empty((B, H * P), dtype=u.dtype, device=u.device), ring, state)
+    y, ring_out, state_out = out
+    _check(load().semicrf_ssm_step(*_rows(u, u.dtype, (B, C)), _param(weight, (C, W)), _param(bias, (C,)),
+                                   *_rows(dt, u.dtype, (B, H)), _param(rate, (H,)), _param(skip, (H,)),
+                                   _param(dt_bias, (H,)), _index(seen, (B,)), _plain(ring, u.dtype, (B, C, W)),
+                                   _param(state, (B, H, P, N)), B, H, P, G, N, W, flags | _act(u),
+                                   _plain(y, u.dtype, (B, H * P)), _plain(ring_out, u.dtype, (B, C, W)),
+                                   _param(state_out, (B, H, P, N)), _stream()))
+    return y

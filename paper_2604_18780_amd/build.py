@@ -7,7 +7,9 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libsemicrf.so")
-SOURCES = [os.path.join(HERE, "csrc", n) for n in ("semicrf.hip", "mscan.hip", "plan.cpp")]
+SOURCES = [os.path.join(HERE, "csrc", n) for n in
+           ("semicrf.hip", "mscan.hip", "plan.cpp", "embed.hip", "conv.hip", "ssm.hip", "ssm_bf16.hip", "ssm_f16.hip",
+            "ssm_f32.hip")]
 OBJDIR = os.path.join(HERE, "_build")
 FLAGS = [
     "-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17",

@@ -1,0 +1,77 @@
+// Shared by the encoder operators (embedding, short convolution, state space scan): storage types of activations,
+// argument checks and the lengths rule.
+#ifndef SEMICRF_ENCODER_H
+#define SEMICRF_ENCODER_H
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "semicrf.h"
+
+namespace semicrf_enc {
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+
+// Elements of a type in the 16 bytes a lane loads at once.
+template <class T> constexpr int PER16 = 16 / (int)sizeof(T);
+
+// n consecutive elements from / to memory that is aligned to their size, as float.  Narrowing rounds to nearest even.
+template <class T, int n> struct Pack {
+    T v[n];
+};
+
+template <class T, int n> __device__ __forceinline__ void load_n(const T *p, float (&o)[n])
+{
+    typedef T V __attribute__((ext_vector_type(n)));
+    const V v = *(const V *)p;
+#pragma unroll
+    for (int e = 0; e < n; ++e) o[e] = (float)v[e];
+}
+
+template <class T, int n> __device__ __forceinline__ void store_n(T *p, const float (&o)[n])
+{
+    typedef T V __attribute__((ext_vector_type(n)));
+    typedef float F __attribute__((ext_vector_type(n)));
+    F f;
+#pragma unroll
+    for (int e = 0; e < n; ++e) f[e] = o[e];
+    *(V *)p = __builtin_convertvector(f, V);
+}
+
+__device__ __forceinline__ int length_of(const int32_t *lengths, int b, int T)
+{
+    if (!lengths) return T;
+    const int L = lengths[b];
+    return L < 0 ? 0 : (L > T ? T : L);
+}
+
+// ln(1 + e^v) without overflow, and its derivative.
+__device__ __forceinline__ float softplus(float v) { return fmaxf(v, 0.0f) + log1pf(expf(-fabsf(v))); }
+__device__ __forceinline__ float sigmoid(float v) { return 1.0f / (1.0f + expf(-v)); }
+
+enum ActType { ACT_F32 = 0, ACT_F16 = 1, ACT_BF16 = 2 };
+
+// The storage type a call's flags name, or -1 where they name two.
+inline int act_type(unsigned flags)
+{
+    const unsigned t = flags & (SEMICRF_EMIS_F16 | SEMICRF_EMIS_BF16);
+    return t == 0 ? ACT_F32 : t == SEMICRF_EMIS_F16 ? ACT_F16 : t == SEMICRF_EMIS_BF16 ? ACT_BF16 : -1;
+}
+inline int act_bytes(int type) { return type == ACT_F32 ? 4 : 2; }
+
+// Rows that are read 16 bytes at a time: base and stride on a 16-byte boundary, at least `width` elements apart.
+inline bool rows_ok(const void *p, int64_t row, int64_t width, int type)
+{
+    return p && ((uintptr_t)p & 15) == 0 && row >= width && row * act_bytes(type) % 16 == 0;
+}
+
+inline int launched() { return hipGetLastError() == hipSuccess ? SEMICRF_OK : SEMICRF_ELAUNCH; }
+
+inline size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+}  // namespace semicrf_enc
+
+#endif

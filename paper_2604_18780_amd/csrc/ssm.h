@@ -1,0 +1,59 @@
+// Selective state space scan: arguments of the kernels, and how a call is cut into pieces.
+//
+//   delta_t = softplus(dt_t + dt_bias),   l_t = delta_t * rate,   u_t = delta_t x_t         (each head)
+//   H_t = e^{l_t} H_{t-1} + u_t B_t^T     [P x N]                 y_t = H_t C_t + skip x_t
+//
+// With c_t = l_1 + ... + l_t the output is a masked product, y_i = sum_{j<=i} e^{c_i-c_j} (C_i . B_j) u_j, and so are the
+// gradients: with G_t the gradient of H_t (G_t = e^{l_{t+1}} G_{t+1} + dy_t C_t^T),
+//   dC_i = sum_{j<=i} e^{c_i-c_j} (dy_i . u_j) B_j      (forwards,  state H)
+//   du_j = sum_{i>=j} e^{c_i-c_j} (B_j . C_i) dy_i      (backwards, state G)
+//   dB_j = sum_{i>=j} e^{c_i-c_j} (u_j . dy_i) C_i      (backwards, state G)
+// All four are one sweep over (query, key, value): blocks of 32 positions as products on the matrix cores, the state from
+// block to block in registers.  Time is cut into segments so that there are waves enough for the chip; states at their
+// boundaries come from a sweep that keeps only the state, chained by k_ssm_chain.
+#ifndef SEMICRF_SSM_H
+#define SEMICRF_SSM_H
+
+#include "encoder.h"
+
+namespace semicrf_enc {
+
+constexpr int BLOCK = 32;  // positions a sweep takes at once
+
+struct SsmArgs {
+    const void *x, *b, *c, *dt, *gy;
+    int64_t x_row, b_row, c_row, dt_row, gy_row;
+    const float *rate, *skip, *dt_bias;
+    const int32_t *lengths;
+    const float *state;       // [B,H,P,N] or null: zeros
+    const float *grad_last;   // [B,H,P,N] or null: gradient of the state after the last token
+    int B, T, H, P, G, N;
+    int seg, nseg;            // positions of a segment (a multiple of BLOCK) and how many there are
+    void *y;
+    int64_t y_row;
+    float *state_out;         // [B,H,P,N] or null
+    void *gx, *gb, *gc, *gdt;
+    int64_t gx_row, gb_row, gc_row, gdt_row;
+    float *grate, *gskip, *gbias, *gstate;
+    // workspace
+    float *hs, *gs;           // [B*H][nseg+1][P][N] states, and gradients of states, at the segments' boundaries
+    float *kept;              // [B*H][nseg] what a state keeps over a segment
+    float *partc, *partb;     // [B*T][H][N] gradients of C and B by head
+    float *rint, *dlin, *qint, *xdu;  // [tiles][B*H][T] see k_ssm_steps
+    float *skipp;             // [tiles][B*H][nseg]
+    double *headp;            // [B*H*nseg][2] sums for rate and bias
+};
+
+enum Use { USE_STATE, USE_Y, USE_DC, USE_DU, USE_DB };
+
+__host__ __device__ inline int tiles_of(int dim) { return dim <= 64 ? 1 : (dim + 63) / 64; }
+
+// one instantiation per storage type, each in a translation unit of its own
+template <class T> int ssm_sweep(Use use, bool rev, const SsmArgs &a, hipStream_t st);
+extern template int ssm_sweep<float>(Use, bool, const SsmArgs &, hipStream_t);
+extern template int ssm_sweep<_Float16>(Use, bool, const SsmArgs &, hipStream_t);
+extern template int ssm_sweep<__bf16>(Use, bool, const SsmArgs &, hipStream_t);
+
+}  // namespace semicrf_enc
+
+#endif

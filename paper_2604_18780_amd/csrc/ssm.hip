@@ -1,0 +1,436 @@
+// Selective state space scan: the small kernels around the sweeps, the single-token form, and the entry points.
+#include "ssm.h"
+
+namespace semicrf_enc {
+
+// States at the segments' boundaries from what each segment adds: H_{s+1} = kept_s H_s + added_s forwards, and the same
+// backwards for gradients of states.  A thread owns four entries.
+template <bool REV> __global__ __launch_bounds__(256) void k_ssm_chain(SsmArgs a)
+{
+    const size_t cells = (size_t)a.P * a.N;
+    const unsigned wide = (unsigned)((cells / 4 + 255) / 256);
+    const size_t at = (size_t)(blockIdx.x % wide * 256 + threadIdx.x) * 4, bh = blockIdx.x / wide;
+    if (at >= cells) return;
+    float *line = (REV ? a.gs : a.hs) + bh * (a.nseg + 1) * cells + at;
+    const float *first = REV ? a.grad_last : a.state;
+    float *last = REV ? a.gstate : a.state_out;
+    const float *kept = a.kept + bh * a.nseg;
+    f4 h = first ? *(const f4 *)(first + bh * cells + at) : (f4)0.0f;
+    *(f4 *)(line + (REV ? (size_t)a.nseg * cells : 0)) = h;
+    constexpr int AHEAD = 8;
+    for (int s0 = 0; s0 < a.nseg; s0 += AHEAD) {
+        f4 added[AHEAD];
+        float k[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (s0 + i < a.nseg) {
+                const int s = REV ? a.nseg - 1 - s0 - i : s0 + i;
+                added[i] = *(const f4 *)(line + (size_t)(REV ? s : s + 1) * cells);
+                k[i] = kept[s];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (s0 + i < a.nseg) {
+                const int s = REV ? a.nseg - 1 - s0 - i : s0 + i;
+                h = k[i] * h + added[i];
+                *(f4 *)(line + (size_t)(REV ? s : s + 1) * cells) = h;
+            }
+        }
+    }
+    if (last) *(f4 *)(last + bh * cells + at) = h;
+}
+
+// Gradients of the steps.  l_t multiplies everything that passes step t: pairs (i, j) with j < t <= i.  A segment is one block
+// here, and the sweeps leave sums of three kinds, so that nothing is ever subtracted:
+//   dlin  pairs with both ends in the block,
+//   rint  pairs that begin before the block, by their end i;        those with i >= t count,
+//   qint  pairs that end behind the block, by their beginning j;    those with j < t count,
+// and the pairs that span the whole block are kept * <G behind it, H before it>.  One wave per (sequence, head, block).
+template <class T> __global__ __launch_bounds__(64) void k_ssm_steps(SsmArgs a)
+{
+    const int lane = threadIdx.x, r = lane & 31;
+    const int seg = blockIdx.x % a.nseg, bh = blockIdx.x / a.nseg, h = bh % a.H, b = bh / a.H;
+    const int L = length_of(a.lengths, b, a.T), t = seg * BLOCK + r;
+    const size_t cells = (size_t)a.P * a.N, lines = (size_t)a.B * a.H * a.T, at = (size_t)bh * a.T + t;
+    const int ntile = tiles_of(a.N), ptile = tiles_of(a.P);
+    T *gdt = (T *)a.gdt + ((int64_t)b * a.T + t) * a.gdt_row + h;
+    const float rate = a.rate[h], bias = a.dt_bias ? a.dt_bias[h] : 0.0f;
+    double across = 0.0, grate = 0.0, gbias = 0.0;
+    if (seg * BLOCK < L) {
+        const f4 *hs = (const f4 *)(a.hs + ((size_t)bh * (a.nseg + 1) + seg) * cells);
+        const f4 *gs = (const f4 *)(a.gs + ((size_t)bh * (a.nseg + 1) + seg + 1) * cells);
+        for (size_t k = lane; k < cells / 4; k += 64) {
+            const f4 p = hs[k], q = gs[k];
+            across += (double)p[0] * q[0] + (double)p[1] * q[1] + (double)p[2] * q[2] + (double)p[3] * q[3];
+        }
+        for (int d = 1; d < 64; d *= 2) across += __shfl_xor(across, d);
+        across *= (double)a.kept[(size_t)bh * a.nseg + seg];
+        const bool in = t < L;
+        float ri = 0.0f, qi = 0.0f, own = 0.0f, dx = 0.0f, raw = 0.0f;
+        if (in) {
+            for (int k = 0; k < ntile; ++k) ri += a.rint[k * lines + at], own += a.dlin[k * lines + at];
+            for (int k = 0; k < ptile; ++k) qi += a.qint[k * lines + at], dx += a.xdu[k * lines + at];
+            raw = (float)((const T *)a.dt)[((int64_t)b * a.T + t) * a.dt_row + h] + bias;
+        }
+        float tail = ri, head = __shfl_up(qi, 1, 32);
+        if (r == 0) head = 0.0f;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const float o = __shfl_down(tail, d, 32), p = __shfl_up(head, d, 32);
+            if (r + d < 32) tail += o;
+            if (r >= d) head += p;
+        }
+        if (in && lane < 32) {
+            const float dl = own + tail + head + (float)across, g = (dx + rate * dl) * sigmoid(raw);
+            const float one[1] = {g};
+            store_n<T, 1>(gdt, one);
+            grate = (double)dl * softplus(raw);
+            gbias = (double)g;
+        }
+        for (int d = 1; d < 32; d *= 2) grate += __shfl_xor(grate, d), gbias += __shfl_xor(gbias, d);
+    }
+    if (lane < 32 && t >= L && t < a.T) *gdt = (T)0.0f;
+    if (lane == 0) {
+        a.headp[2 * (size_t)blockIdx.x] = grate;
+        a.headp[2 * (size_t)blockIdx.x + 1] = gbias;
+    }
+}
+
+// Sums over sequences and segments, in a fixed order.  One workgroup per head.
+__global__ __launch_bounds__(256) void k_ssm_params(SsmArgs a)
+{
+    __shared__ double s[3][256];
+    const int h = blockIdx.x, tid = threadIdx.x;
+    double rate = 0.0, bias = 0.0, skip = 0.0;
+    const int n = a.B * a.nseg, ptile = tiles_of(a.P);
+    for (int k = tid; k < n; k += 256) {
+        const size_t at = ((size_t)(k / a.nseg) * a.H + h) * a.nseg + k % a.nseg;
+        rate += a.headp[2 * at];
+        bias += a.headp[2 * at + 1];
+        for (int p = 0; p < ptile; ++p) skip += (double)a.skipp[(size_t)p * a.B * a.H * a.nseg + at];
+    }
+    s[0][tid] = rate, s[1][tid] = bias, s[2][tid] = skip;
+    for (int d = 128; d > 0; d /= 2) {
+        __syncthreads();
+        if (tid < d)
+            for (int k = 0; k < 3; ++k) s[k][tid] += s[k][tid + d];
+    }
+    if (tid == 0) {
+        a.grate[h] = (float)s[0][0];
+        if (a.gbias) a.gbias[h] = (float)s[1][0];
+        if (a.gskip) a.gskip[h] = (float)s[2][0];
+    }
+}
+
+// Gradients of B and C: the sum over the heads that share them.  A thread owns four columns of a row.
+template <class T> __global__ __launch_bounds__(256) void k_ssm_heads(SsmArgs a)
+{
+    const int quads = a.N / 4, per = a.H / a.G;
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, rows = (int64_t)a.B * a.T;
+    if (at >= rows * a.G * quads) return;
+    const int q = (int)(at % quads), grp = (int)(at / quads % a.G);
+    const int64_t row = at / quads / a.G;
+    const int b = (int)(row / a.T), t = (int)(row % a.T);
+    const float *part = blockIdx.y ? a.partc : a.partb;
+    T *out = (T *)(blockIdx.y ? a.gc : a.gb) + row * (blockIdx.y ? a.gc_row : a.gb_row) + grp * a.N + 4 * q;
+    f4 s = (f4)0.0f;
+    if (t < length_of(a.lengths, b, a.T))
+        for (int h = 0; h < per; ++h) s += *(const f4 *)(part + (row * a.H + grp * per + h) * a.N + 4 * q);
+    const float o[4] = {s[0], s[1], s[2], s[3]};
+    store_n<T, 4>(out, o);
+}
+
+// ---- one more token of each stream --------------------------------------------------------------------------------
+
+struct StepArgs {
+    const void *u, *dt, *ring;
+    int64_t u_row, dt_row;
+    const float *weight, *bias, *rate, *skip, *dt_bias, *state;
+    const int32_t *seen;
+    int B, H, P, G, N, W;
+    void *y, *ring_out;
+    float *state_out;
+    bool linear;
+};
+
+constexpr int STEP_ROWS = 16;  // rows of a head's state that a workgroup owns
+
+// One launch for the whole step: a workgroup owns 16 rows of one head's [P x N] state (16 lanes a row), and convolves what it
+// needs for them: its 16 channels of x and its group's B and C, again in every workgroup of the group (2 N W multiply-adds)
+// rather than in a launch before this one.  The ring holds the last W tokens at slot (position mod W), so the one slot that
+// is written is the one nobody reads.
+// Bound by the state, read and written once; the loads are on their way before the convolution starts.
+template <class T> __global__ __launch_bounds__(256) void k_ssm_step(StepArgs a)
+{
+    __shared__ float sx[STEP_ROWS], sb[128], sc[128];
+    const int tid = threadIdx.x, tiles = (a.P + STEP_ROWS - 1) / STEP_ROWS;
+    const int tile = blockIdx.x % tiles, h = blockIdx.x / tiles % a.H, b = blockIdx.x / tiles / a.H;
+    const int grp = h / (a.H / a.G), channels = a.H * a.P + 2 * a.G * a.N;
+    const int p = tile * STEP_ROWS + tid / 16, q = tid % 16;
+    const size_t cell = (((size_t)b * a.H + h) * a.P + p) * a.N;
+    f4 s[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int n = 4 * (q + 16 * k);
+        if (p < a.P && n < a.N) s[k] = *(const f4 *)(a.state + cell + n);
+    }
+    const int seen = a.seen[b], W = a.W;
+    const bool live = seen >= 0;
+    const float raw = live ? (float)((const T *)a.dt)[b * a.dt_row + h] + (a.dt_bias ? a.dt_bias[h] : 0.0f) : 0.0f;
+    const int slot = live ? seen % W : -1;
+    for (int k = tid; k < STEP_ROWS + 2 * a.N; k += 256) {
+        int ch;
+        float *to;
+        bool mine = true;  // whether this workgroup writes the channel's ring
+        if (k < STEP_ROWS) {
+            if (tile * STEP_ROWS + k >= a.P) continue;
+            ch = h * a.P + tile * STEP_ROWS + k;
+            to = sx + k;
+        } else {
+            const int n = (k - STEP_ROWS) % a.N, which = (k - STEP_ROWS) / a.N;
+            ch = a.H * a.P + (which * a.G + grp) * a.N + n;
+            to = (which ? sc : sb) + n;
+            mine = tile == 0 && h % (a.H / a.G) == 0;
+        }
+        const T *ring = (const T *)a.ring + ((size_t)b * channels + ch) * W;
+        T *ring_out = (T *)a.ring_out + ((size_t)b * channels + ch) * W;
+        const T fresh = live ? ((const T *)a.u)[b * a.u_row + ch] : (T)0.0f;
+        float v = a.bias ? a.bias[ch] : 0.0f;
+        for (int j = 0; j < W; ++j) {
+            // slot j holds the newest position up to `seen` that is j mod W
+            const int back = live ? (slot - j + W) % W : 0;
+            const T held = j == slot ? fresh : ring[j];
+            if (live && back <= seen) v += a.weight[ch * W + W - 1 - back] * (float)held;
+            if (mine && (ring_out != ring || j == slot)) ring_out[j] = held;
+        }
+        *to = a.linear ? v : v * sigmoid(v);
+    }
+    __syncthreads();
+    const float delta = softplus(raw), keep = expf(delta * a.rate[h]);
+    const float x = p < a.P ? sx[tid / 16] : 0.0f, u = delta * x;
+    float y = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int n = 4 * (q + 16 * k);
+        if (p < a.P && n < a.N) {
+            if (live) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[k][e] = s[k][e] * keep + u * sb[n + e];
+                    y += s[k][e] * sc[n + e];
+                }
+            }
+            if (live || a.state_out != a.state) *(f4 *)(a.state_out + cell + n) = s[k];
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) y += __shfl_xor(y, d);
+    if (q == 0 && p < a.P) {
+        const float o[1] = {live ? y + (a.skip ? a.skip[h] : 0.0f) * x : 0.0f};
+        store_n<T, 1>((T *)a.y + ((size_t)b * a.H + h) * a.P + p, o);
+    }
+}
+
+// ---- planning -----------------------------------------------------------------------------------------------------
+
+struct SsmPlan {
+    int seg, nseg;
+    size_t hs, gs, kept, partc, partb, rint, dlin, qint, xdu, skipp, headp, total;
+};
+
+// Positions of a segment.  A wave walks a segment block by block, so what counts is that there are waves enough: four for
+// each SIMD of the chip (1024 SIMDs).  Below 128 positions the states at the boundaries (16 KB for P = N = 64, against 256
+// bytes of x and y a position) would cost more than the waves bring.  A backward call needs the states at
+// every block, for the gradients of the steps.
+int segment_length(int B, int T, int H, int tiles, bool grad)
+{
+    const long waves = (long)B * H * tiles, want = 4096;
+    long seg = ((long)T * waves + want - 1) / want;
+    if (seg < 128) seg = 128;
+    if (grad) seg = BLOCK;
+    const long whole = ((long)T + BLOCK - 1) / BLOCK * BLOCK;
+    seg = (seg + BLOCK - 1) / BLOCK * BLOCK;
+    return (int)(seg < whole ? seg : whole);
+}
+
+int make_ssm_plan(int B, int T, int H, int P, int G, int N, bool grad, SsmPlan *p)
+{
+    if (B < 1 || T < 1 || H < 1 || P < 1 || G < 1 || N < 1 || H % G) return SEMICRF_EINVAL;
+    if (P % 8 || N % 8 || P > 128 || N > 128 || T > (1 << 30) || (double)B * T * H > 2e9) return SEMICRF_EUNSUPPORTED;
+    p->seg = segment_length(B, T, H, tiles_of(P), grad);
+    p->nseg = (T + p->seg - 1) / p->seg;
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t o = at;
+        at += align256(bytes);
+        return o;
+    };
+    const size_t bh = (size_t)B * H, cells = (size_t)P * N, rows = (size_t)B * T;
+    const bool chain = grad || p->nseg > 1;
+    p->hs = take(chain ? bh * (p->nseg + 1) * cells * 4 : 0);
+    p->kept = take(chain ? bh * p->nseg * 4 : 0);
+    if (grad) {
+        p->gs = take(bh * (p->nseg + 1) * cells * 4);
+        p->partc = take(rows * H * N * 4);
+        p->partb = take(rows * H * N * 4);
+        p->rint = take(tiles_of(N) * rows * H * 4);
+        p->dlin = take(tiles_of(N) * rows * H * 4);
+        p->qint = take(tiles_of(P) * rows * H * 4);
+        p->xdu = take(tiles_of(P) * rows * H * 4);
+        p->skipp = take(tiles_of(P) * bh * p->nseg * 4);
+        p->headp = take(bh * p->nseg * 16);
+    }
+    p->total = at;
+    return SEMICRF_OK;
+}
+
+int sweep(int type, Use use, bool rev, const SsmArgs &a, hipStream_t st)
+{
+    if (type == ACT_BF16) return ssm_sweep<__bf16>(use, rev, a, st);
+    if (type == ACT_F16) return ssm_sweep<_Float16>(use, rev, a, st);
+    return ssm_sweep<float>(use, rev, a, st);
+}
+
+int chain(bool rev, const SsmArgs &a, hipStream_t st)
+{
+    const dim3 g((unsigned)((a.P * a.N / 4 + 255) / 256 * a.B * a.H)), t(256);
+    if (rev) hipLaunchKernelGGL((k_ssm_chain<true>), g, t, 0, st, a);
+    else hipLaunchKernelGGL((k_ssm_chain<false>), g, t, 0, st, a);
+    return launched();
+}
+
+int ssm_inputs(SsmArgs &a, int type, const void *x, int64_t x_row, const void *b, int64_t b_row, const void *c,
+               int64_t c_row, const void *dt, int64_t dt_row, const float *rate, const float *skip,
+               const float *dt_bias, const int32_t *lengths, const float *state, int B, int T, int H, int P, int G, int N)
+{
+    if (type < 0 || !dt || !rate || dt_row < H || ((uintptr_t)state & 15)) return SEMICRF_EINVAL;
+    if (!rows_ok(x, x_row, (int64_t)H * P, type) || !rows_ok(b, b_row, (int64_t)G * N, type) ||
+        !rows_ok(c, c_row, (int64_t)G * N, type))
+        return SEMICRF_EINVAL;
+    a.x = x; a.b = b; a.c = c; a.dt = dt;
+    a.x_row = x_row; a.b_row = b_row; a.c_row = c_row; a.dt_row = dt_row;
+    a.rate = rate; a.skip = skip; a.dt_bias = dt_bias; a.lengths = lengths; a.state = state;
+    a.B = B; a.T = T; a.H = H; a.P = P; a.G = G; a.N = N;
+    return SEMICRF_OK;
+}
+
+}  // namespace semicrf_enc
+
+using namespace semicrf_enc;
+
+extern "C" {
+
+int semicrf_ssm_workspace_bytes(int B, int T, int H, int P, int G, int N, int want_grad, size_t *bytes)
+{
+    if (!bytes) return SEMICRF_EINVAL;
+    SsmPlan p = {};
+    const int rc = make_ssm_plan(B, T, H, P, G, N, want_grad != 0, &p);
+    if (rc == SEMICRF_OK) *bytes = p.total;
+    return rc;
+}
+
+int semicrf_ssm_fwd(const void *x, int64_t x_row, const void *b, int64_t b_row, const void *c, int64_t c_row,
+                    const void *dt, int64_t dt_row, const float *rate, const float *skip, const float *dt_bias,
+                    const int32_t *lengths, const float *state, int B, int T, int H, int P, int G, int N,
+                    unsigned flags, void *workspace, size_t workspace_bytes, void *y, int64_t y_row,
+                    float *state_out, void *stream)
+{
+    SsmPlan p = {};
+    if (int rc = make_ssm_plan(B, T, H, P, G, N, false, &p)) return rc;
+    const int type = act_type(flags);
+    SsmArgs a = {};
+    if (int rc = ssm_inputs(a, type, x, x_row, b, b_row, c, c_row, dt, dt_row, rate, skip, dt_bias, lengths, state, B, T, H,
+                            P, G, N))
+        return rc;
+    if (!rows_ok(y, y_row, (int64_t)H * P, type) || ((uintptr_t)state_out & 15)) return SEMICRF_EINVAL;
+    if (p.total && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < p.total)) return SEMICRF_EWORKSPACE;
+    a.y = y; a.y_row = y_row; a.state_out = state_out;
+    a.seg = p.seg; a.nseg = p.nseg;
+    const hipStream_t st = (hipStream_t)stream;
+    if (p.nseg > 1) {
+        a.hs = (float *)((char *)workspace + p.hs);
+        a.kept = (float *)((char *)workspace + p.kept);
+        if (int rc = sweep(type, USE_STATE, false, a, st)) return rc;
+        if (int rc = chain(false, a, st)) return rc;
+    }
+    return sweep(type, USE_Y, false, a, st);
+}
+
+int semicrf_ssm_bwd(const void *x, int64_t x_row, const void *b, int64_t b_row, const void *c, int64_t c_row,
+                    const void *dt, int64_t dt_row, const float *rate, const float *skip, const float *dt_bias,
+                    const int32_t *lengths, const float *state, const void *grad_y, int64_t grad_y_row,
+                    const float *grad_state_out, int B, int T, int H, int P, int G, int N, unsigned flags,
+                    void *workspace, size_t workspace_bytes, void *grad_x, int64_t grad_x_row, void *grad_b,
+                    int64_t grad_b_row, void *grad_c, int64_t grad_c_row, void *grad_dt, int64_t grad_dt_row,
+                    float *grad_rate, float *grad_skip, float *grad_dt_bias, float *grad_state, void *stream)
+{
+    SsmPlan p = {};
+    if (int rc = make_ssm_plan(B, T, H, P, G, N, true, &p)) return rc;
+    const int type = act_type(flags);
+    SsmArgs a = {};
+    if (int rc = ssm_inputs(a, type, x, x_row, b, b_row, c, c_row, dt, dt_row, rate, skip, dt_bias, lengths, state, B, T, H,
+                            P, G, N))
+        return rc;
+    if (!rows_ok(grad_y, grad_y_row, (int64_t)H * P, type) || !rows_ok(grad_x, grad_x_row, (int64_t)H * P, type) ||
+        !rows_ok(grad_b, grad_b_row, (int64_t)G * N, type) || !rows_ok(grad_c, grad_c_row, (int64_t)G * N, type) ||
+        !grad_dt || grad_dt_row < H || !grad_rate || ((uintptr_t)grad_state_out & 15) || ((uintptr_t)grad_state & 15))
+        return SEMICRF_EINVAL;
+    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < p.total) return SEMICRF_EWORKSPACE;
+    a.gy = grad_y; a.gy_row = grad_y_row; a.grad_last = grad_state_out;
+    a.gx = grad_x; a.gx_row = grad_x_row; a.gb = grad_b; a.gb_row = grad_b_row; a.gc = grad_c; a.gc_row = grad_c_row;
+    a.gdt = grad_dt; a.gdt_row = grad_dt_row;
+    a.grate = grad_rate; a.gskip = grad_skip; a.gbias = grad_dt_bias; a.gstate = grad_state;
+    a.seg = p.seg; a.nseg = p.nseg;
+    char *w = (char *)workspace;
+    a.hs = (float *)(w + p.hs); a.gs = (float *)(w + p.gs); a.kept = (float *)(w + p.kept);
+    a.partc = (float *)(w + p.partc); a.partb = (float *)(w + p.partb);
+    a.rint = (float *)(w + p.rint); a.dlin = (float *)(w + p.dlin); a.qint = (float *)(w + p.qint);
+    a.xdu = (float *)(w + p.xdu); a.skipp = (float *)(w + p.skipp); a.headp = (double *)(w + p.headp);
+    const hipStream_t st = (hipStream_t)stream;
+    if (int rc = sweep(type, USE_STATE, false, a, st)) return rc;
+    if (int rc = sweep(type, USE_STATE, true, a, st)) return rc;
+    if (int rc = chain(false, a, st)) return rc;
+    if (int rc = chain(true, a, st)) return rc;
+    if (int rc = sweep(type, USE_DC, false, a, st)) return rc;
+    if (int rc = sweep(type, USE_DU, true, a, st)) return rc;
+    if (int rc = sweep(type, USE_DB, true, a, st)) return rc;
+    const dim3 steps(B * H * p.nseg), heads((unsigned)(((int64_t)B * T * G * (N / 4) + 255) / 256), 2);
+    if (type == ACT_BF16) {
+        hipLaunchKernelGGL((k_ssm_steps<__bf16>), steps, dim3(64), 0, st, a);
+        hipLaunchKernelGGL((k_ssm_heads<__bf16>), heads, dim3(256), 0, st, a);
+    } else if (type == ACT_F16) {
+        hipLaunchKernelGGL((k_ssm_steps<_Float16>), steps, dim3(64), 0, st, a);
+        hipLaunchKernelGGL((k_ssm_heads<_Float16>), heads, dim3(256), 0, st, a);
+    } else {
+        hipLaunchKernelGGL((k_ssm_steps<float>), steps, dim3(64), 0, st, a);
+        hipLaunchKernelGGL((k_ssm_heads<float>), heads, dim3(256), 0, st, a);
+    }
+    hipLaunchKernelGGL(k_ssm_params, dim3(H), dim3(256), 0, st, a);
+    return launched();
+}
+
+int semicrf_ssm_step(const void *u, int64_t u_row, const float *weight, const float *bias, const void *dt, int64_t dt_row,
+                     const float *rate, const float *skip, const float *dt_bias, const int32_t *seen, const void *ring,
+                     const float *state, int B, int H, int P, int G, int N, int W, unsigned flags, void *y,
+                     void *ring_out, float *state_out, void *stream)
+{
+    if (B < 1 || H < 1 || P < 1 || G < 1 || N < 1 || H % G || W < 1) return SEMICRF_EINVAL;
+    const int64_t channels = (int64_t)H * P + 2 * (int64_t)G * N;
+    const int tiles = (P + STEP_ROWS - 1) / STEP_ROWS, type = act_type(flags);
+    if (P % 8 || N % 8 || P > 128 || N > 128 || W > 4 || (double)B * H * tiles > 2e9 || channels > 1e8)
+        return SEMICRF_EUNSUPPORTED;
+    if (type < 0 || !u || u_row < channels || !weight || !dt || dt_row < H || !rate || !seen || !ring || !state || !y ||
+        !ring_out || !state_out || (((uintptr_t)state | (uintptr_t)state_out) & 15))
+        return SEMICRF_EINVAL;
+    StepArgs a = {u, dt, ring, u_row, dt_row, weight, bias, rate, skip, dt_bias, state, seen, B, H, P, G, N, W,
+                  y, ring_out, state_out, (flags & SEMICRF_CONV_LINEAR) != 0};
+    const dim3 g((unsigned)(B * H * tiles)), t(256);
+    const hipStream_t st = (hipStream_t)stream;
+    if (type == ACT_BF16) hipLaunchKernelGGL((k_ssm_step<__bf16>), g, t, 0, st, a);
+    else if (type == ACT_F16) hipLaunchKernelGGL((k_ssm_step<_Float16>), g, t, 0, st, a);
+    else hipLaunchKernelGGL((k_ssm_step<float>), g, t, 0, st, a);
+    return launched();
+}
+
+}  // extern "C"
