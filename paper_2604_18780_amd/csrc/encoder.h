@@ -48,9 +48,28 @@ __device__ __forceinline__ int length_of(const int32_t *lengths, int b, int T)
     return L < 0 ? 0 : (L > T ? T : L);
 }
 
+// e^v to the rounding of its result (the hardware's power of two, with the rounding of its argument made good).
+__device__ __forceinline__ float exp_of(float v)
+{
+    const float h = v * 1.44269504f, l = __builtin_fmaf(v, 1.44269504f, -h) + v * 1.92596299e-8f;
+    const float e = __builtin_amdgcn_exp2f(h);
+    return __builtin_fmaf(e, l * 0.693147181f, e);
+}
+
 // ln(1 + e^v) without overflow, and its derivative.
-__device__ __forceinline__ float softplus(float v) { return fmaxf(v, 0.0f) + log1pf(expf(-fabsf(v))); }
-__device__ __forceinline__ float sigmoid(float v) { return 1.0f / (1.0f + expf(-v)); }
+__device__ __forceinline__ float softplus(float v)
+{
+    const float e = exp_of(fmaxf(-fabsf(v), -100.0f)), u = 1.0f + e;
+    // for small e the series, to 2^-27 of its value; else the logarithm, with what 1 + e has lost put back
+    const float small = e * __builtin_fmaf(e, __builtin_fmaf(e, __builtin_fmaf(e, __builtin_fmaf(e, 0.2f, -0.25f), 0.333333333f), -0.5f), 1.0f);
+    const float large = __builtin_fmaf(e - (u - 1.0f), __builtin_amdgcn_rcpf(u), 0.693147181f * __builtin_amdgcn_logf(u));
+    return fmaxf(v, 0.0f) + (e < 0.03125f ? small : large);
+}
+__device__ __forceinline__ float sigmoid(float v)
+{
+    const float e = exp_of(fmaxf(-fabsf(v), -100.0f));
+    return (v < 0.0f ? e : 1.0f) / (1.0f + e);
+}
 
 enum ActType { ACT_F32 = 0, ACT_F16 = 1, ACT_BF16 = 2 };
 
@@ -62,10 +81,11 @@ inline int act_type(unsigned flags)
 }
 inline int act_bytes(int type) { return type == ACT_F32 ? 4 : 2; }
 
-// Rows that are read 16 bytes at a time: base and stride on a 16-byte boundary, at least `width` elements apart.
+// Rows that are read 16 bytes at a time: base and stride on a 16-byte boundary, at least `width` elements apart, and so little that
+// 64 of them are within a 32-bit offset.
 inline bool rows_ok(const void *p, int64_t row, int64_t width, int type)
 {
-    return p && ((uintptr_t)p & 15) == 0 && row >= width && row * act_bytes(type) % 16 == 0;
+    return p && ((uintptr_t)p & 15) == 0 && row >= width && row <= (1 << 22) && row * act_bytes(type) % 16 == 0;
 }
 
 inline int launched() { return hipGetLastError() == hipSuccess ? SEMICRF_OK : SEMICRF_ELAUNCH; }

@@ -53,6 +53,10 @@ template <class T> int ssm_sweep(Use use, bool rev, const SsmArgs &a, hipStream_
 extern template int ssm_sweep<float>(Use, bool, const SsmArgs &, hipStream_t);
 extern template int ssm_sweep<_Float16>(Use, bool, const SsmArgs &, hipStream_t);
 extern template int ssm_sweep<__bf16>(Use, bool, const SsmArgs &, hipStream_t);
+template <class T> int ssm_scan(bool out, bool rev, const SsmArgs &a, hipStream_t st);
+extern template int ssm_scan<float>(bool, bool, const SsmArgs &, hipStream_t);
+extern template int ssm_scan<_Float16>(bool, bool, const SsmArgs &, hipStream_t);
+extern template int ssm_scan<__bf16>(bool, bool, const SsmArgs &, hipStream_t);
 
 }  // namespace semicrf_enc
 

@@ -239,18 +239,14 @@ struct SsmPlan {
     size_t hs, gs, kept, partc, partb, rint, dlin, qint, xdu, skipp, headp, total;
 };
 
-// Positions of a segment.  A wave walks a segment block by block, so what counts is that there are waves enough: four for
-// each SIMD of the chip (1024 SIMDs).  Below 128 positions the states at the boundaries (16 KB for P = N = 64, against 256
-// bytes of x and y a position) would cost more than the waves bring.  A backward call needs the states at
-// every block, for the gradients of the steps.
-int segment_length(int B, int T, int H, int tiles, bool grad)
+// Positions of a segment of a forward call.
+int segment_length(int B, int T, int H)
 {
-    const long waves = (long)B * H * tiles, want = 4096;
-    long seg = ((long)T * waves + want - 1) / want;
-    if (seg < 128) seg = 128;
-    if (grad) seg = BLOCK;
-    const long whole = ((long)T + BLOCK - 1) / BLOCK * BLOCK;
-    seg = (seg + BLOCK - 1) / BLOCK * BLOCK;
+    const long groups = (long)B * H, want = 1536;
+    long seg = ((long)T * groups + want - 1) / want;
+    if (seg < 256) seg = 256;
+    const long whole = ((long)T + 63) / 64 * 64;
+    seg = (seg + 63) / 64 * 64;
     return (int)(seg < whole ? seg : whole);
 }
 
@@ -258,7 +254,7 @@ int make_ssm_plan(int B, int T, int H, int P, int G, int N, bool grad, SsmPlan *
 {
     if (B < 1 || T < 1 || H < 1 || P < 1 || G < 1 || N < 1 || H % G) return SEMICRF_EINVAL;
     if (P % 8 || N % 8 || P > 128 || N > 128 || T > (1 << 30) || (double)B * T * H > 2e9) return SEMICRF_EUNSUPPORTED;
-    p->seg = segment_length(B, T, H, tiles_of(P), grad);
+    p->seg = grad ? BLOCK : segment_length(B, T, H);
     p->nseg = (T + p->seg - 1) / p->seg;
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -290,6 +286,13 @@ int sweep(int type, Use use, bool rev, const SsmArgs &a, hipStream_t st)
     if (type == ACT_BF16) return ssm_sweep<__bf16>(use, rev, a, st);
     if (type == ACT_F16) return ssm_sweep<_Float16>(use, rev, a, st);
     return ssm_sweep<float>(use, rev, a, st);
+}
+
+int scan(int type, bool out, bool rev, const SsmArgs &a, hipStream_t st)
+{
+    if (type == ACT_BF16) return ssm_scan<__bf16>(out, rev, a, st);
+    if (type == ACT_F16) return ssm_scan<_Float16>(out, rev, a, st);
+    return ssm_scan<float>(out, rev, a, st);
 }
 
 int chain(bool rev, const SsmArgs &a, hipStream_t st)
@@ -351,10 +354,10 @@ int semicrf_ssm_fwd(const void *x, int64_t x_row, const void *b, int64_t b_row, 
     if (p.nseg > 1) {
         a.hs = (float *)((char *)workspace + p.hs);
         a.kept = (float *)((char *)workspace + p.kept);
-        if (int rc = sweep(type, USE_STATE, false, a, st)) return rc;
+        if (int rc = scan(type, false, false, a, st)) return rc;
         if (int rc = chain(false, a, st)) return rc;
     }
-    return sweep(type, USE_Y, false, a, st);
+    return scan(type, true, false, a, st);
 }
 
 int semicrf_ssm_bwd(const void *x, int64_t x_row, const void *b, int64_t b_row, const void *c, int64_t c_row,

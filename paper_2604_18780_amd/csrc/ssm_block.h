@@ -1,0 +1,243 @@
+// Blocks of positions in LDS: staging of operands' rows, their fragments, and the steps of a block.
+#ifndef SEMICRF_SSM_BLOCK_H
+#define SEMICRF_SSM_BLOCK_H
+
+#include "ssm_ops.h"
+
+namespace semicrf_enc {
+
+// Rows of one sequence behind a range check: what lies beyond `bytes` reads as zeros and is not written.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const void *base, int64_t bytes)
+{
+    const int n = bytes < 0 ? 0 : bytes > 0x7ffffff0 ? 0x7ffffff0 : (int)bytes;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, n, 0x00020000);
+}
+constexpr uint32_t OUTSIDE = 0x80000000u;  // an offset beyond any range
+
+// One operand's rows of a block: Q rows of `dim` elements, staged as bfloat16 parts W wide (padding columns zeros), by NT
+// threads.  REV: row r is the block's position Q-1-r.
+// A row is W/4 cells of 8 bytes; cell c lies at c ^ mix(row), so that neither the sixteen rows a row-wise read takes side by side
+// nor the four rows by four cells of a transposed one meet in a bank.
+template <class T, int Q, int W, int NT, bool REV> struct Tile {
+    static constexpr int RAW = Parts<T>::raw, E = PER16<T>, PART = Q * W, ELEMS = RAW * PART;
+    static constexpr int PR = W / E, ALL = Q * PR, CH = (ALL + NT - 1) / NT;
+    const T *base;   // the sequence's first row, at the head's or group's columns
+    int64_t row;
+    uint32_t off[CH];
+    u4 r[CH];
+    static __device__ __forceinline__ int mix(int rw)
+    {
+        const int low = (rw >> 2) & 3;
+        return W >= 64 ? ((rw & 3) << 2) | low : W == 32 ? ((rw & 2) << 1) | low : low;
+    }
+    // element `col` (a multiple of 4) of row rw
+    static __device__ __forceinline__ int cell(int rw, int col) { return rw * W + (((col >> 2) ^ mix(rw)) << 2); }
+    __device__ __forceinline__ void init(const T *b, int64_t rw, int dim, int tid)
+    {
+        base = b;
+        row = rw;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int at = tid + NT * i, k = at / PR, col = at % PR * E;
+            off[i] = k < Q && col < dim ? (uint32_t)((REV ? Q - 1 - k : k) * row + col) * (uint32_t)sizeof(T) : OUTSIDE;
+        }
+    }
+    __device__ __forceinline__ void fetch(int t, int L)
+    {
+        const __amdgpu_buffer_rsrc_t rows = rows_from(base + t * row, (L - t) * row * (int64_t)sizeof(T));
+#pragma unroll
+        for (int i = 0; i < CH; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b128(rows, (int)off[i], 0, 0);
+    }
+    __device__ __forceinline__ void put(__bf16 *tile, int tid) const
+    {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int at = tid + NT * i, k = at / PR, col = at % PR * E;
+            if (ALL % NT != 0 && at >= ALL) break;
+            __bf16 *to = tile + cell(k, col);
+            if constexpr (RAW == 1) {
+                *(u2 *)to = (u2){r[i][0], r[i][1]};
+                *(u2 *)(tile + cell(k, col + 4)) = (u2){r[i][2], r[i][3]};
+            } else if constexpr (RAW == 2) {
+                typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+                const Op<2> o = split<2>(__builtin_convertvector(__builtin_bit_cast(h8, r[i]), f8));
+                __bf16 *next = tile + cell(k, col + 4);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const u4 v = __builtin_bit_cast(u4, o.p[j]);
+                    *(u2 *)(to + j * PART) = (u2){v[0], v[1]};
+                    *(u2 *)(next + j * PART) = (u2){v[2], v[3]};
+                }
+            } else {
+                const f4 v = __builtin_bit_cast(f4, r[i]);
+                float x[4] = {v[0], v[1], v[2], v[3]};
+                uint32_t p[3][2];
+                split_pairs<3, 2>(x, p);
+#pragma unroll
+                for (int j = 0; j < 3; ++j) *(u2 *)(to + j * PART) = (u2){p[j][0], p[j][1]};
+            }
+        }
+    }
+    // inner index = column: columns at + 4g.., at + 16 + 4g.. of a row
+    static __device__ __forceinline__ Op<RAW> by_row(const __bf16 *tile, int rw, int at, int g)
+    {
+        Op<RAW> o;
+        const __bf16 *p = tile + cell(rw, at + 4 * g), *q = tile + cell(rw, at + 16 + 4 * g);
+#pragma unroll
+        for (int k = 0; k < RAW; ++k)
+            o.p[k] = __builtin_shufflevector(*(const bf4 *)(p + k * PART), *(const bf4 *)(q + k * PART), 0, 1, 2, 3, 4, 5, 6, 7);
+        return o;
+    }
+    // inner index = row: rows first + 4g.., first + 16 + 4g.. of column at + lane % 16
+    static __device__ __forceinline__ Op<RAW> by_col(const __bf16 *tile, int first, int at, int lane)
+    {
+        typedef __attribute__((address_space(3))) s4 *lds;
+        Op<RAW> o;
+        // rows sixteen apart are mixed alike
+        __bf16 *p = const_cast<__bf16 *>(tile) + cell(first + (lane >> 2), at + 4 * (lane & 3));
+#pragma unroll
+        for (int k = 0; k < RAW; ++k) {
+            const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(p + k * PART));
+            const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(p + k * PART + 16 * W));
+            o.p[k] = __builtin_shufflevector(__builtin_bit_cast(bf4, lo), __builtin_bit_cast(bf4, hi), 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+        return o;
+    }
+};
+
+// The values an operand's parts stand for.
+template <int n> __device__ __forceinline__ f8 values(const Op<n> &o)
+{
+    f8 v = __builtin_convertvector(o.p[n - 1], f8);
+#pragma unroll
+    for (int k = n - 2; k >= 0; --k) v += __builtin_convertvector(o.p[k], f8);
+    return v;
+}
+
+__device__ __forceinline__ float pow2(double v) { return __builtin_amdgcn_exp2f((float)v); }
+
+// Steps of a block of Q positions.  c is log2 of what is kept from the block's start to a position (REV: from its far end in
+// time, without the position's own step).  What is kept between two positions is 2^(c_i - c_j): between different sixteens it is
+// taken as query[i] * from[.][j], the two sides of the query's sixteen's first c, neither of which can overflow.
+template <int Q> struct Steps {
+    double c[Q];
+    float out[Q];               // 2^c
+    float in[Q];                // what the state at the block's other end keeps of a position's term, times its scale
+    float key[Q];               // scale of a position's term
+    float delta[Q];
+    float step[Q];              // what is kept from the position before
+    float query[Q];             // 2^(c_i - c of the first of its sixteen)
+    float from[Q / 16 - 1][Q];  // 2^(c of the first of sixteen k+1 - c_j) * key_j, for earlier j
+    double total;               // log2 of what the block keeps
+};
+
+// The value of another lane of the wave, by a fixed pattern; 0 where the pattern or the mask of rows of sixteen names none.
+template <int CTRL, int ROWS> __device__ __forceinline__ double other(double v)
+{
+    const u2 x = __builtin_bit_cast(u2, v);
+    const u2 y = {(uint32_t)__builtin_amdgcn_update_dpp(0, (int)x[0], CTRL, ROWS, 0xf, true),
+                  (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x[1], CTRL, ROWS, 0xf, true)};
+    return __builtin_bit_cast(double, y);
+}
+__device__ __forceinline__ double of_lane(double v, int lane)
+{
+    const u2 x = __builtin_bit_cast(u2, v);
+    const u2 y = {(uint32_t)__builtin_amdgcn_readlane((int)x[0], lane), (uint32_t)__builtin_amdgcn_readlane((int)x[1], lane)};
+    return __builtin_bit_cast(double, y);
+}
+
+// One wave; lane = row (Q = 32: the upper half of the wave repeats nothing and writes nothing).
+template <int Q, bool REV> __device__ __forceinline__ void make_steps(Steps<Q> &s, float dt, float bias, float rate, bool scaled, int lane)
+{
+    // a step beyond the sequence's end has delta = 0: nothing comes in and nothing is forgotten
+    const float raw = dt + bias, delta = raw == -INFINITY ? 0.0f : softplus(raw);
+    const double l = (double)delta * (double)rate * 1.4426950408889634;
+    double c = l, step = l;
+    if (REV) step = other<0x138, 0xf>(l);  // of the lane below: handed back in time, a state passes the later step
+    c += other<0x111, 0xf>(c);  // from 1, 2, 4, 8 lanes below in a row of sixteen
+    c += other<0x112, 0xf>(c);
+    c += other<0x114, 0xf>(c);
+    c += other<0x118, 0xf>(c);
+    c += other<0x142, 0xa>(c);  // the last of the row before, for rows 1 and 3
+    if (Q == 64) c += other<0x143, 0xc>(c);  // lane 31, for rows 2 and 3
+    const double total = of_lane(c, Q - 1);
+    if (REV) c -= l;
+    const float key = scaled ? delta : 1.0f;
+    double first = of_lane(c, 0);
+    float from[Q / 16 - 1];
+#pragma unroll
+    for (int k = 0; k < Q / 16 - 1; ++k) {
+        const double ref = of_lane(c, 16 * (k + 1));
+        if (lane >= 16 * (k + 1)) first = ref;
+        from[k] = lane < 16 * (k + 1) ? pow2(ref - c) * key : 0.0f;
+    }
+    if (lane < Q) {
+        s.c[lane] = c;
+        s.out[lane] = pow2(c);
+        s.in[lane] = pow2(total - c) * key;
+        s.key[lane] = key;
+        s.delta[lane] = delta;
+        s.step[lane] = pow2(step);
+        s.query[lane] = pow2(c - first);
+#pragma unroll
+        for (int k = 0; k < Q / 16 - 1; ++k) s.from[k][lane] = from[k];
+        if (lane == 0) s.total = total;
+    }
+}
+
+// Scores of a block: sixteen queries `it`, sixteen keys `jt` <= it, as four keys of one query in a lane.  Where the two are the
+// same sixteen, only the last of a lane's keys takes a power; the earlier ones multiply what is kept on the way to it.
+template <int Q> __device__ __forceinline__ f4 weigh(const Steps<Q> &s, f4 m, int it, int jt, int i16, int g)
+{
+    if (jt < it) return m * *(const f4 *)(s.from[it - 1] + 16 * jt + 4 * g) * s.query[16 * it + i16];
+    const f4 key = *(const f4 *)(s.key + 16 * it + 4 * g), step = *(const f4 *)(s.step + 16 * it + 4 * g);
+    const float last = fminf((float)(s.c[16 * it + i16] - s.c[16 * it + 4 * g + 3]), 0.0f);
+    f4 e;
+    e[3] = i16 >= 4 * g + 3 ? __builtin_amdgcn_exp2f(last) : 0.0f;
+#pragma unroll
+    for (int r = 2; r >= 0; --r) e[r] = i16 == 4 * g + r ? 1.0f : e[r + 1] * step[r + 1];
+    return m * (e * key);
+}
+
+// Where scores are handed from the wave that makes them to those that multiply with them: operands of queries 16 it.., keys
+// 32 ks.., ks <= it / 2; each is two tiles of sixteen keys, of which the second may lie behind the queries (zeros).
+template <int Q, int MADE> struct Scores {
+    static constexpr int IT = Q / 16, TILES = IT * (IT + 1) / 2, OPS = IT == 4 ? 6 : 2, ELEMS = OPS * MADE * 64 * 8;
+    static constexpr __device__ __host__ int op(int it, int ks) { return it < 2 ? it : 2 * it - 2 + ks; }
+    // tile k of the block, and the wave of NW that makes it: with four waves three, three, two and two, sixteen keys each
+    static constexpr __device__ int query(int k) { return IT == 2 ? (k > 0) : k == 0 ? 0 : k == 1 || k == 3 ? 1 : k == 4 || k == 6 || k == 9 ? 2 : 3; }
+    static constexpr __device__ int keys(int k) { return IT == 2 ? k / 2 : k < 3 || k == 9 ? 0 : k < 6 ? 1 : k < 8 ? 2 : 3; }
+    static constexpr __device__ int wave(int k, int nw) { return IT == 4 && nw == 4 ? (k == 9 ? 3 : keys(k)) : k % nw; }
+    static __device__ __forceinline__ void put(__bf16 *sm, int it, int jt, f4 v, int lane)
+    {
+        float x[4] = {v[0], v[1], v[2], v[3]};
+        uint32_t p[MADE][2];
+        split_pairs<MADE, 2>(x, p);
+#pragma unroll
+        for (int k = 0; k < MADE; ++k)
+            *(u2 *)(sm + ((op(it, jt / 2) * MADE + k) * 64 + lane) * 8 + 4 * (jt & 1)) = (u2){p[k][0], p[k][1]};
+    }
+    // zeros where an operand's second tile lies behind its queries; once, by the whole workgroup
+    static __device__ __forceinline__ void clear(__bf16 *sm, int tid, int nt)
+    {
+        for (int k = tid; k < ELEMS / 8; k += nt) *(u4 *)(sm + 8 * k) = (u4)0u;
+    }
+    static __device__ __forceinline__ Op<MADE> get(const __bf16 *sm, int m, int lane)
+    {
+        Op<MADE> o;
+#pragma unroll
+        for (int k = 0; k < MADE; ++k) o.p[k] = *(const bf8 *)(sm + ((m * MADE + k) * 64 + lane) * 8);
+        return o;
+    }
+};
+
+__device__ __forceinline__ void lds_barrier()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+}  // namespace semicrf_enc
+
+#endif

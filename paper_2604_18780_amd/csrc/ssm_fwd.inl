@@ -1,0 +1,215 @@
+// The scan over one segment of one head, forwards (outputs, or the state alone) and backwards in time (the state alone): see ssm.h
+// for the mathematics.
+//
+// A workgroup owns a segment of one head and takes it in blocks of Q positions; a wave owns sixteen channels: their columns of
+// the state (N x 16, in registers from block to block) and of the output.  Rows of the block are staged in LDS as they lie in
+// memory, the next block's already on their way; what the products need with positions as the inner index is read transposed
+// (ds_read_b64_tr_b16).
+//   scores  M[j,i] = (B_j . C_i) e^{c_i-c_j} delta_j, j <= i, skip added where j = i; each wave makes some, all read them
+//   output  O[p,i] = sum_j x[j,p] M[j,i] + e^{c_i} sum_n S[n,p] C[i,n]
+//   state   S[n,p] = e^{c_Q} S[n,p] + sum_j B[j,n] (e^{c_Q-c_j} delta_j x[j,p])
+// Steps (delta, c) are made for four blocks at a time, one by each wave.
+#ifndef SEMICRF_SSM_FWD_INL
+#define SEMICRF_SSM_FWD_INL
+
+#include "ssm_block.h"
+
+namespace semicrf_enc {
+
+template <class T, int Q, int DK, int PV, bool OUT, bool REV> __global__ __launch_bounds__(PV * 4, 2) void k_ssm_scan(SsmArgs a)
+{
+    constexpr int NT = PV * 4, NW = PV / 16, KT = DK / 16, KS = DK / 32, IT = Q / 16, QS = Q / 32;
+    constexpr int AHEAD = NW < 4 ? NW : 4;  // blocks whose steps are made together, one by each wave
+    constexpr int RAW = Parts<T>::raw, MADE = Parts<T>::made, HELD = 3;
+    typedef Tile<T, Q, DK, NT, REV> TK;
+    typedef Tile<T, Q, PV, NT, REV> TV;
+    typedef Scores<Q, MADE> SC;
+    __shared__ __attribute__((aligned(16))) __bf16 sq[OUT ? TK::ELEMS : 8];
+    __shared__ __attribute__((aligned(16))) __bf16 sk[TK::ELEMS];
+    __shared__ __attribute__((aligned(16))) __bf16 sv[TV::ELEMS];
+    __shared__ __attribute__((aligned(16))) __bf16 sm[OUT ? SC::ELEMS : 8];
+    __shared__ __attribute__((aligned(16))) Steps<Q> ss[AHEAD];
+
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, i16 = lane & 15;
+    // heads of one segment follow each other on one XCD (workgroups go round the eight in turn): they share B and C
+    const int unit = (blockIdx.x % 8) + 8 * (blockIdx.x / 8 / a.H), h = blockIdx.x / 8 % a.H;
+    if (unit >= a.B * a.nseg) return;
+    const int b = unit / a.nseg, seg = unit % a.nseg, grp = h / (a.H / a.G), bh = b * a.H + h;
+    const int L = __builtin_amdgcn_readfirstlane(length_of(a.lengths, b, a.T));
+    const int t0 = seg * a.seg, t1 = t0 + a.seg < a.T ? t0 + a.seg : a.T;
+    const int used = (t1 < L ? t1 : L) - t0, nblk = used > 0 ? (used + Q - 1) / Q : 0;
+    const size_t cells = (size_t)a.P * a.N;
+    const int64_t rb = (int64_t)b * a.T;
+
+    TK rq, rk;
+    TV rv;
+    const T *qb = (const T *)a.c + rb * a.c_row + grp * a.N, *kb = (const T *)a.b + rb * a.b_row + grp * a.N;
+    if constexpr (OUT) rq.init(qb, a.c_row, a.N, tid);
+    rk.init(REV ? qb : kb, REV ? a.c_row : a.b_row, a.N, tid);
+    rv.init((REV ? (const T *)a.gy + rb * a.gy_row : (const T *)a.x + rb * a.x_row) + h * a.P, REV ? a.gy_row : a.x_row, a.P, tid);
+    const float rate = a.rate[h], bias = a.dt_bias ? a.dt_bias[h] : 0.0f, skip = OUT && a.skip ? a.skip[h] : 0.0f;
+    const T *dts = (const T *)a.dt + rb * a.dt_row + h;
+
+    // state: rows n (16 kt + 4g + r), column p = 16 w + lane % 16; memory is [P][N]
+    const int p = 16 * w + i16;
+    f4 S[KT];
+    const float *from = !OUT ? nullptr : a.hs ? a.hs + ((size_t)bh * (a.nseg + 1) + seg) * cells
+                                              : a.state ? a.state + bh * cells : nullptr;
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) {
+        const int n = 16 * kt + 4 * g;
+        S[kt] = from && n < a.N && p < a.P ? *(const f4 *)(from + (size_t)p * a.N + n) : (f4)0.0f;
+    }
+
+    double gone = 0.0;
+    auto at = [&](int n) { return t0 + Q * (REV ? nblk - 1 - n : n); };
+    auto dt_of = [&](int n) {
+        const int r = lane % Q, t = at(n) + (REV ? Q - 1 - r : r);
+        return n < nblk && t < L ? (float)dts[t * a.dt_row] : -INFINITY;
+    };
+    const uint32_t y_off = 16 * w + 4 * g < a.P ? (uint32_t)(i16 * a.y_row + 16 * w + 4 * g) * (uint32_t)sizeof(T) : OUTSIDE;
+    f4 skips;  // on the diagonal of the scores
+#pragma unroll
+    for (int r = 0; r < 4; ++r) skips[r] = 4 * g + r == i16 ? skip : 0.0f;
+    float dt_next = dt_of(w);  // of the block this wave makes the steps of
+    if (nblk) {
+        if constexpr (OUT) rq.fetch(at(0), L);
+        rk.fetch(at(0), L);
+        rv.fetch(at(0), L);
+        if constexpr (OUT) SC::clear(sm, tid, NT);
+    }
+    for (int n = 0; n < nblk; ++n) {
+        const int base = at(n);
+        const Steps<Q> &s = ss[n % AHEAD];
+        if (n % AHEAD == 0 && w < AHEAD) {
+            make_steps<Q, REV>(ss[w], dt_next, bias, rate, !REV, lane);
+            dt_next = dt_of(n + AHEAD + w);
+        }
+        if constexpr (OUT) rq.put(sq, tid);
+        rk.put(sk, tid);
+        rv.put(sv, tid);
+        lds_barrier();
+        if (n + 1 < nblk) {
+            if constexpr (OUT) rq.fetch(at(n + 1), L);
+            rk.fetch(at(n + 1), L);
+            rv.fetch(at(n + 1), L);
+        }
+        f4 O[IT];
+        if constexpr (OUT) {
+            Op<RAW> q[IT][KS];
+#pragma unroll
+            for (int it = 0; it < IT; ++it)
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) q[it][ks] = TK::by_row(sq, 16 * it + i16, 32 * ks, g);
+#pragma unroll
+            for (int k = 0; k < SC::TILES; ++k) {
+                if (SC::wave(k, NW) != w) continue;
+                const int it = SC::query(k), jt = SC::keys(k);
+                f4 m = (f4)0.0f;
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) m = mma(m, TK::by_row(sk, 16 * jt + i16, 32 * ks, g), q[it][ks]);
+                m = weigh(s, m, it, jt, i16, g);
+                if (it == jt) m += skips;
+                SC::put(sm, it, jt, m, lane);
+            }
+            // what the state at the block's start gives
+#pragma unroll
+            for (int it = 0; it < IT; ++it) O[it] = (f4)0.0f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const Op<MADE> st = split<MADE>(__builtin_shufflevector(S[2 * ks], S[2 * ks + 1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                for (int it = 0; it < IT; ++it) O[it] = mma(O[it], st, q[it][ks]);
+            }
+#pragma unroll
+            for (int it = 0; it < IT; ++it) O[it] *= s.out[16 * it + i16];
+        }
+        Op<RAW> v[QS];
+#pragma unroll
+        for (int ks = 0; ks < QS; ++ks) v[ks] = TV::by_col(sv, 32 * ks, 16 * w, lane);
+        // the state at the block's end
+        {
+            const float keep = pow2(s.total);
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) S[kt] *= keep;
+#pragma unroll
+            for (int ks = 0; ks < QS; ++ks) {
+                const f4 lo = *(const f4 *)(s.in + 32 * ks + 4 * g), hi = *(const f4 *)(s.in + 32 * ks + 16 + 4 * g);
+                const Op<HELD> u = split<HELD>(values(v[ks]) * __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) S[kt] = mma(S[kt], TK::by_col(sk, 32 * ks, 16 * kt, lane), u);
+            }
+            gone += s.total;
+        }
+        lds_barrier();
+        if constexpr (OUT) {
+#pragma unroll
+            for (int it = 0; it < IT; ++it)
+#pragma unroll
+                for (int ks = 0; ks <= it / 2; ++ks) O[it] = mma(O[it], v[ks], SC::get(sm, SC::op(it, ks), lane));
+            // a lane holds channels 16 w + 4g .. +3 of positions i16, 16 + i16, ..
+            const __amdgpu_buffer_rsrc_t rows = rows_from((const T *)a.y + (rb + base) * a.y_row + h * a.P, (t1 - base) * a.y_row * (int64_t)sizeof(T));
+#pragma unroll
+            for (int it = 0; it < IT; ++it) {
+                typedef T T4 __attribute__((ext_vector_type(4)));
+                const T4 o = __builtin_convertvector(O[it], T4);
+                const int from_row = (int)(16 * it * a.y_row * (int64_t)sizeof(T));
+                if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, o), rows, (int)y_off, from_row, 0);
+                else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u2, o), rows, (int)y_off, from_row, 0);
+            }
+        }
+    }
+
+    float *to;
+    if constexpr (!OUT) {
+        to = REV ? a.gs + ((size_t)bh * (a.nseg + 1) + seg) * cells : a.hs + ((size_t)bh * (a.nseg + 1) + seg + 1) * cells;
+        if (tid == 0) a.kept[(size_t)bh * a.nseg + seg] = pow2(gone);
+    } else {
+        to = !a.hs && a.state_out ? a.state_out + bh * cells : nullptr;
+    }
+    if (to) {
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+            const int n = 16 * kt + 4 * g;
+            if (n < a.N && p < a.P) *(f4 *)(to + (size_t)p * a.N + n) = S[kt];
+        }
+    }
+    if constexpr (OUT) {
+        // rows beyond the sequence's end that no block covered
+        const int first = t0 + nblk * Q, wide = a.P / 4;
+        for (int k = tid; k < (t1 - first) * wide; k += NT) {
+            const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            store_n<T, 4>((T *)a.y + (rb + first + k / wide) * a.y_row + h * a.P + k % wide * 4, zero);
+        }
+    }
+}
+
+template <class T, int Q, int DK, int PV> int launch_scan(bool out, bool rev, const SsmArgs &a, hipStream_t st)
+{
+    const long grid = ((long)a.B * a.nseg + 7) / 8 * 8 * a.H;
+    if (grid > 0x7fffffffL) return SEMICRF_EUNSUPPORTED;
+    const dim3 g((unsigned)grid), t(PV * 4);
+    if (out) hipLaunchKernelGGL((k_ssm_scan<T, Q, DK, PV, true, false>), g, t, 0, st, a);
+    else if (!rev) hipLaunchKernelGGL((k_ssm_scan<T, Q, DK, PV, false, false>), g, t, 0, st, a);
+    else hipLaunchKernelGGL((k_ssm_scan<T, Q, DK, PV, false, true>), g, t, 0, st, a);
+    return launched();
+}
+template <class T, int DK> int launch_scan_p(bool out, bool rev, const SsmArgs &a, hipStream_t st)
+{
+    // blocks of 64 as long as the staged parts leave room for two workgroups on a compute unit
+    constexpr int R = Parts<T>::raw;
+    if (a.P <= 16) return launch_scan<T, R * (2 * DK + 16) <= 448 ? 64 : 32, DK, 16>(out, rev, a, st);
+    if (a.P <= 32) return launch_scan<T, R * (2 * DK + 32) <= 448 ? 64 : 32, DK, 32>(out, rev, a, st);
+    if (a.P <= 64) return launch_scan<T, R * (2 * DK + 64) <= 448 ? 64 : 32, DK, 64>(out, rev, a, st);
+    return launch_scan<T, R * (2 * DK + 128) <= 448 ? 64 : 32, DK, 128>(out, rev, a, st);
+}
+template <class T> int ssm_scan(bool out, bool rev, const SsmArgs &a, hipStream_t st)
+{
+    if (a.N <= 32) return launch_scan_p<T, 32>(out, rev, a, st);
+    if (a.N <= 64) return launch_scan_p<T, 64>(out, rev, a, st);
+    return launch_scan_p<T, 128>(out, rev, a, st);
+}
+
+}  // namespace semicrf_enc
+
+#endif

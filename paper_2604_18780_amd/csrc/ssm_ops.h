@@ -1,0 +1,150 @@
+// Operands of the scan's products on the matrix cores.
+//
+// The matrix cores multiply bfloat16.  Operands that are wider are split into bfloat16 parts whose sum holds 8, 16 or 24
+// bits, and the products of parts that matter are added up in 32 bits: bfloat16 inputs are exact in one part, float16 in two,
+// float32 takes three.  What is computed on the way takes two or three, by what it goes into: two leave 2^-17 of a term, which
+// is less than the rounding of an output stored in two bytes; states and the gradients of the steps, whose sums are returned
+// in 32 bits, take three (2^-25).
+//
+// With g = lane / 16, a lane holds rows 4g..4g+3 of one column of a 16 x 16 result, and eight inner indexes of one row (or column)
+// of an operand: any eight, as long as both operands hold the same.  They are 4g..4g+3 of each of two tiles of 16, so that two
+// results stacked are an operand as they stand.
+#ifndef SEMICRF_SSM_OPS_H
+#define SEMICRF_SSM_OPS_H
+
+#include "ssm.h"
+
+namespace semicrf_enc {
+
+typedef __bf16 bf4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+
+template <class T> struct Parts;  // of an input, and of what goes only into outputs of this type
+template <> struct Parts<__bf16> { static constexpr int raw = 1, made = 2; };
+template <> struct Parts<_Float16> { static constexpr int raw = 2, made = 2; };
+template <> struct Parts<float> { static constexpr int raw = 3, made = 3; };
+
+template <int n> struct Op { bf8 p[n]; };
+
+// Two floats rounded to bfloat16 (to nearest even), the first in the lower half.
+__device__ __forceinline__ uint32_t round2(float a, float b)
+{
+    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    uint32_t o = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){a, b}, bf2));
+    asm("" : "+v"(o));  // one conversion for the pair: without this each value is rounded again for its remainder
+    return o;
+}
+
+// n parts of 2 m values: v = p[0] + p[1] + ..
+template <int n, int m> __device__ __forceinline__ void split_pairs(float (&v)[2 * m], uint32_t (&o)[n][m])
+{
+#pragma unroll
+    for (int i = 0; i < n; ++i)
+#pragma unroll
+        for (int k = 0; k < m; ++k) {
+            o[i][k] = round2(v[2 * k], v[2 * k + 1]);
+            if (i + 1 < n) {
+                v[2 * k] -= __builtin_bit_cast(float, o[i][k] << 16);
+                v[2 * k + 1] -= __builtin_bit_cast(float, o[i][k] & 0xffff0000u);
+            }
+        }
+}
+
+template <int n> __device__ __forceinline__ Op<n> split(f8 v)
+{
+    float a[8] = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+    uint32_t p[n][4];
+    split_pairs<n, 4>(a, p);
+    Op<n> o;
+#pragma unroll
+    for (int i = 0; i < n; ++i) o.p[i] = __builtin_bit_cast(bf8, (u4){p[i][0], p[i][1], p[i][2], p[i][3]});
+    return o;
+}
+
+template <int n> __device__ __forceinline__ Op<n> zero_op()
+{
+    Op<n> o;
+#pragma unroll
+    for (int i = 0; i < n; ++i) o.p[i] = (bf8)(__bf16)0.0f;
+    return o;
+}
+
+template <int na, int nb> __device__ __forceinline__ f4 mma(f4 acc, const Op<na> &a, const Op<nb> &b)
+{
+    constexpr int most = na > nb ? na : nb;
+#pragma unroll
+    for (int i = na - 1; i >= 0; --i)
+#pragma unroll
+        for (int j = nb - 1; j >= 0; --j)
+            if (i + j < most) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[j], acc, 0, 0, 0);
+    return acc;
+}
+
+// ---- operands from a staged tile ----------------------------------------------------------------------------------
+
+// inner index = column: columns at+4g.., at+16+4g.. of row `row`
+template <class T> __device__ __forceinline__ f8 row_floats(const T *row, int at, int g)
+{
+    float a[4], b[4];
+    load_n<T, 4>(row + at + 4 * g, a);
+    load_n<T, 4>(row + at + 16 + 4 * g, b);
+    return f8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+}
+template <class T> __device__ __forceinline__ Op<Parts<T>::raw> row_op(const T *row, int at, int g)
+{
+    if constexpr (sizeof(T) == 2 && Parts<T>::raw == 1) {
+        const bf4 a = *(const bf4 *)(row + at + 4 * g), b = *(const bf4 *)(row + at + 16 + 4 * g);
+        Op<1> o;
+        o.p[0] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        return o;
+    } else {
+        return split<Parts<T>::raw>(row_floats<T>(row, at, g));
+    }
+}
+
+// inner index = row: rows 4g.., 16+4g.. of column `at` + lane % 16
+template <class T, int S> __device__ __forceinline__ void col_raw(const T *tile, int at, int lane, T (&o)[8])
+{
+    const int g = lane >> 4, i = lane & 15;
+    if constexpr (sizeof(T) == 2) {
+        typedef __attribute__((address_space(3))) s4 *lds;
+        T *p = const_cast<T *>(tile) + (4 * g + (i >> 2)) * S + at + 4 * (i & 3);
+        const s4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(p));
+        const s4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(p + 16 * S));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            o[e] = __builtin_bit_cast(T, (short)a[e]);
+            o[4 + e] = __builtin_bit_cast(T, (short)b[e]);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            o[e] = tile[(4 * g + e) * S + at + i];
+            o[4 + e] = tile[(16 + 4 * g + e) * S + at + i];
+        }
+    }
+}
+template <class T, int S> __device__ __forceinline__ f8 col_floats(const T *tile, int at, int lane)
+{
+    T o[8];
+    col_raw<T, S>(tile, at, lane, o);
+    return f8{(float)o[0], (float)o[1], (float)o[2], (float)o[3], (float)o[4], (float)o[5], (float)o[6], (float)o[7]};
+}
+template <class T, int S> __device__ __forceinline__ Op<Parts<T>::raw> col_op(const T *tile, int at, int lane)
+{
+    if constexpr (sizeof(T) == 2 && Parts<T>::raw == 1) {
+        T o[8];
+        col_raw<T, S>(tile, at, lane, o);
+        Op<1> r;
+        r.p[0] = bf8{o[0], o[1], o[2], o[3], o[4], o[5], o[6], o[7]};
+        return r;
+    } else {
+        return split<Parts<T>::raw>(col_floats<T, S>(tile, at, lane));
+    }
+}
+
+}  // namespace semicrf_enc
+
+#endif

@@ -7,120 +7,9 @@
 //   state   S[k,v] = e^{c_32} S[k,v] + sum_j w_j K[j,k] V[j,v]
 // The rows a lane holds of a 16 x 16 result are the inner indexes it holds of the next product's operand (4g..4g+3 of each
 // of two tiles, g = lane / 16), so scores and state go from one product into the next without leaving registers.
-//
-// The matrix cores multiply bfloat16.  Operands that are wider are split into bfloat16 parts whose sum holds 8, 16 or 24
-// bits, and the products of parts that matter are added up in 32 bits: bfloat16 inputs are exact in one part, float16
-// in two, float32 takes three; what is computed (weighed scores and keys, the state) takes two, three for float32, which
-// leaves 2^-17 (2^-25) of a term: less than the outputs' own rounding, and little enough that final states and parameter
-// gradients, which are returned in 32 bits, hold five digits.  Where the state goes into the gradients of the steps it takes
-// three for all types.
-#include "ssm.h"
+#include "ssm_block.h"
 
 namespace semicrf_enc {
-
-typedef __bf16 bf4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
-typedef short s4 __attribute__((ext_vector_type(4)));
-
-template <class T> struct Parts;
-template <> struct Parts<__bf16> { static constexpr int raw = 1, made = 2; };
-template <> struct Parts<_Float16> { static constexpr int raw = 2, made = 2; };
-template <> struct Parts<float> { static constexpr int raw = 3, made = 3; };
-
-template <int n> struct Op { bf8 p[n]; };
-
-template <int n> __device__ __forceinline__ Op<n> split(f8 v)
-{
-    Op<n> o;
-#pragma unroll
-    for (int i = 0; i < n; ++i) {
-        o.p[i] = __builtin_convertvector(v, bf8);
-        if (i + 1 < n) v -= __builtin_convertvector(o.p[i], f8);
-    }
-    return o;
-}
-
-template <int n> __device__ __forceinline__ Op<n> zero_op()
-{
-    Op<n> o;
-#pragma unroll
-    for (int i = 0; i < n; ++i) o.p[i] = (bf8)(__bf16)0.0f;
-    return o;
-}
-
-template <int na, int nb> __device__ __forceinline__ f4 mma(f4 acc, const Op<na> &a, const Op<nb> &b)
-{
-    constexpr int most = na > nb ? na : nb;
-#pragma unroll
-    for (int i = na - 1; i >= 0; --i)
-#pragma unroll
-        for (int j = nb - 1; j >= 0; --j)
-            if (i + j < most) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[j], acc, 0, 0, 0);
-    return acc;
-}
-
-// ---- operands from a staged tile ----------------------------------------------------------------------------------
-
-// inner index = column: columns at+4g.., at+16+4g.. of row `row`
-template <class T> __device__ __forceinline__ f8 row_floats(const T *row, int at, int g)
-{
-    float a[4], b[4];
-    load_n<T, 4>(row + at + 4 * g, a);
-    load_n<T, 4>(row + at + 16 + 4 * g, b);
-    return f8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-}
-template <class T> __device__ __forceinline__ Op<Parts<T>::raw> row_op(const T *row, int at, int g)
-{
-    if constexpr (sizeof(T) == 2 && Parts<T>::raw == 1) {
-        const bf4 a = *(const bf4 *)(row + at + 4 * g), b = *(const bf4 *)(row + at + 16 + 4 * g);
-        Op<1> o;
-        o.p[0] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-        return o;
-    } else {
-        return split<Parts<T>::raw>(row_floats<T>(row, at, g));
-    }
-}
-
-// inner index = row: rows 4g.., 16+4g.. of column `at` + lane % 16
-template <class T, int S> __device__ __forceinline__ void col_raw(const T *tile, int at, int lane, T (&o)[8])
-{
-    const int g = lane >> 4, i = lane & 15;
-    if constexpr (sizeof(T) == 2) {
-        typedef __attribute__((address_space(3))) s4 *lds;
-        T *p = const_cast<T *>(tile) + (4 * g + (i >> 2)) * S + at + 4 * (i & 3);
-        const s4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(p));
-        const s4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(p + 16 * S));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            o[e] = __builtin_bit_cast(T, (short)a[e]);
-            o[4 + e] = __builtin_bit_cast(T, (short)b[e]);
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            o[e] = tile[(4 * g + e) * S + at + i];
-            o[4 + e] = tile[(16 + 4 * g + e) * S + at + i];
-        }
-    }
-}
-template <class T, int S> __device__ __forceinline__ f8 col_floats(const T *tile, int at, int lane)
-{
-    T o[8];
-    col_raw<T, S>(tile, at, lane, o);
-    return f8{(float)o[0], (float)o[1], (float)o[2], (float)o[3], (float)o[4], (float)o[5], (float)o[6], (float)o[7]};
-}
-template <class T, int S> __device__ __forceinline__ Op<Parts<T>::raw> col_op(const T *tile, int at, int lane)
-{
-    if constexpr (sizeof(T) == 2 && Parts<T>::raw == 1) {
-        T o[8];
-        col_raw<T, S>(tile, at, lane, o);
-        Op<1> r;
-        r.p[0] = bf8{o[0], o[1], o[2], o[3], o[4], o[5], o[6], o[7]};
-        return r;
-    } else {
-        return split<Parts<T>::raw>(col_floats<T, S>(tile, at, lane));
-    }
-}
 
 // ---- staging ------------------------------------------------------------------------------------------------------
 
@@ -150,7 +39,7 @@ template <class T, int W> struct Rows {
     }
 };
 
-struct Steps {  // of one block, by row of the staged tiles
+struct Steps32 {  // of one block, by row of the staged tiles
     double c[BLOCK];      // log2 of what has been kept up to a query
     float out[BLOCK];     // e^c
     float in[BLOCK];      // what the state at the block's end keeps of a key, times the key's scale
@@ -158,7 +47,7 @@ struct Steps {  // of one block, by row of the staged tiles
     float query[BLOCK];   // the query's scale
 };
 
-__device__ __forceinline__ float pow2(double v) { return __builtin_amdgcn_exp2f((float)v); }
+
 
 template <class T, int DK, int DV, Use USE, bool REV>
 __global__ __launch_bounds__(64) void k_ssm_sweep(SsmArgs a)
@@ -174,7 +63,7 @@ __global__ __launch_bounds__(64) void k_ssm_sweep(SsmArgs a)
     __shared__ __attribute__((aligned(16))) T sk[BLOCK * SK];
     __shared__ __attribute__((aligned(16))) T sv[BLOCK * SV];
     __shared__ __attribute__((aligned(16))) T se[EXTRA ? BLOCK * SV : 8];
-    __shared__ Steps ss;
+    __shared__ Steps32 ss;
 
     const int lane = threadIdx.x, g = lane >> 4, i16 = lane & 15;
     const int vdim = WIDE_N ? a.N : a.P, kdim = WIDE_N ? a.P : a.N;
