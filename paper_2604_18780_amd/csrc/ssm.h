@@ -8,17 +8,15 @@
 //   dC_i = sum_{j<=i} e^{c_i-c_j} (dy_i . u_j) B_j      (forwards,  state H)
 //   du_j = sum_{i>=j} e^{c_i-c_j} (B_j . C_i) dy_i      (backwards, state G)
 //   dB_j = sum_{i>=j} e^{c_i-c_j} (u_j . dy_i) C_i      (backwards, state G)
-// All four are one sweep over (query, key, value): blocks of 32 positions as products on the matrix cores, the state from
-// block to block in registers.  Time is cut into segments so that there are waves enough for the chip; states at their
-// boundaries come from a sweep that keeps only the state, chained by k_ssm_chain.
+// Blocks of positions go through the matrix cores, the state from block to block in registers.  Time is cut into segments so that
+// there are workgroups enough for the chip; states at their boundaries come from a scan that keeps only the state, chained by
+// k_ssm_chain.
 #ifndef SEMICRF_SSM_H
 #define SEMICRF_SSM_H
 
 #include "encoder.h"
 
 namespace semicrf_enc {
-
-constexpr int BLOCK = 32;  // positions a sweep takes at once
 
 struct SsmArgs {
     const void *x, *b, *c, *dt, *gy;
@@ -28,7 +26,10 @@ struct SsmArgs {
     const float *state;       // [B,H,P,N] or null: zeros
     const float *grad_last;   // [B,H,P,N] or null: gradient of the state after the last token
     int B, T, H, P, G, N;
-    int seg, nseg;            // positions of a segment (a multiple of BLOCK) and how many there are
+    int seg, nseg;            // positions of a segment (a multiple of 64) and how many there are
+    int c_heads, c_chunks;    // heads of a group that a workgroup of k_ssm_grad_c takes, and how many such there are
+    int b_heads, b_chunks;    // of k_ssm_grad_xb
+    int block;                // positions of a block of the gradient kernels
     void *y;
     int64_t y_row;
     float *state_out;         // [B,H,P,N] or null
@@ -38,25 +39,24 @@ struct SsmArgs {
     // workspace
     float *hs, *gs;           // [B*H][nseg+1][P][N] states, and gradients of states, at the segments' boundaries
     float *kept;              // [B*H][nseg] what a state keeps over a segment
-    float *partc, *partb;     // [B*T][H][N] gradients of C and B by head
-    float *rint, *dlin, *qint, *xdu;  // [tiles][B*H][T] see k_ssm_steps
-    float *skipp;             // [tiles][B*H][nseg]
+    float *partc, *partb;     // [chunks][B*T][G][N] gradients of C and B by workgroup, where there are several
+    float *rint, *dlin, *qint, *xdu;  // [B*H][T] see k_ssm_steps
+    float *skipp;             // [B*H][nseg]
     double *headp;            // [B*H*nseg][2] sums for rate and bias
 };
 
-enum Use { USE_STATE, USE_Y, USE_DC, USE_DU, USE_DB };
-
-__host__ __device__ inline int tiles_of(int dim) { return dim <= 64 ? 1 : (dim + 63) / 64; }
+// Positions of a block of the gradient kernels: what their four staged operands (of `raw` parts, `dim` wide) leave room for.
+constexpr int grad_block(int raw, int dim) { return raw * dim <= 64 ? 64 : 32; }
 
 // one instantiation per storage type, each in a translation unit of its own
-template <class T> int ssm_sweep(Use use, bool rev, const SsmArgs &a, hipStream_t st);
-extern template int ssm_sweep<float>(Use, bool, const SsmArgs &, hipStream_t);
-extern template int ssm_sweep<_Float16>(Use, bool, const SsmArgs &, hipStream_t);
-extern template int ssm_sweep<__bf16>(Use, bool, const SsmArgs &, hipStream_t);
 template <class T> int ssm_scan(bool out, bool rev, const SsmArgs &a, hipStream_t st);
 extern template int ssm_scan<float>(bool, bool, const SsmArgs &, hipStream_t);
 extern template int ssm_scan<_Float16>(bool, bool, const SsmArgs &, hipStream_t);
 extern template int ssm_scan<__bf16>(bool, bool, const SsmArgs &, hipStream_t);
+template <class T> int ssm_grad(const SsmArgs &a, hipStream_t st);
+extern template int ssm_grad<float>(const SsmArgs &, hipStream_t);
+extern template int ssm_grad<_Float16>(const SsmArgs &, hipStream_t);
+extern template int ssm_grad<__bf16>(const SsmArgs &, hipStream_t);
 
 }  // namespace semicrf_enc
 

@@ -41,56 +41,67 @@ template <bool REV> __global__ __launch_bounds__(256) void k_ssm_chain(SsmArgs a
     if (last) *(f4 *)(last + bh * cells + at) = h;
 }
 
-// Gradients of the steps.  l_t multiplies everything that passes step t: pairs (i, j) with j < t <= i.  A segment is one block
-// here, and the sweeps leave sums of three kinds, so that nothing is ever subtracted:
-//   dlin  pairs with both ends in the block,
-//   rint  pairs that begin before the block, by their end i;        those with i >= t count,
-//   qint  pairs that end behind the block, by their beginning j;    those with j < t count,
-// and the pairs that span the whole block are kept * <G behind it, H before it>.  One wave per (sequence, head, block).
+// Gradients of the steps.  l_t multiplies everything that passes step t: pairs (i, j) with j < t <= i, of four kinds by block:
+//   dlin[t]  both ends in t's block,
+//   rint[i]  from before the block to i in it; those with i >= t count,
+//   qint[j]  from j in the block to behind it; those with j < t count,
+//   across   from before the block to behind it.
+// At a segment's end all pairs that cross it are <G, H>; from there backwards, taking off those that begin in a block leaves
+// its `across`, and adding those that end in it gives what crosses its start.  Where a block keeps less than 2^-30, nothing
+// is left of the difference but its rounding: `across` is 0.  One wave per (sequence, head, segment).
 template <class T> __global__ __launch_bounds__(64) void k_ssm_steps(SsmArgs a)
 {
-    const int lane = threadIdx.x, r = lane & 31;
+    const int lane = threadIdx.x, Q = a.block, r = lane & (Q - 1);
     const int seg = blockIdx.x % a.nseg, bh = blockIdx.x / a.nseg, h = bh % a.H, b = bh / a.H;
-    const int L = length_of(a.lengths, b, a.T), t = seg * BLOCK + r;
-    const size_t cells = (size_t)a.P * a.N, lines = (size_t)a.B * a.H * a.T, at = (size_t)bh * a.T + t;
-    const int ntile = tiles_of(a.N), ptile = tiles_of(a.P);
-    T *gdt = (T *)a.gdt + ((int64_t)b * a.T + t) * a.gdt_row + h;
+    const int L = length_of(a.lengths, b, a.T);
+    const int t0 = seg * a.seg, t1 = t0 + a.seg < a.T ? t0 + a.seg : a.T;
+    const int used = (t1 < L ? t1 : L) - t0, nblk = used > 0 ? (used + Q - 1) / Q : 0;
+    const size_t cells = (size_t)a.P * a.N;
+    T *gdt = (T *)a.gdt + (int64_t)b * a.T * a.gdt_row + h;
+    const T *dts = (const T *)a.dt + (int64_t)b * a.T * a.dt_row + h;
     const float rate = a.rate[h], bias = a.dt_bias ? a.dt_bias[h] : 0.0f;
     double across = 0.0, grate = 0.0, gbias = 0.0;
-    if (seg * BLOCK < L) {
-        const f4 *hs = (const f4 *)(a.hs + ((size_t)bh * (a.nseg + 1) + seg) * cells);
+    if (nblk) {
+        const f4 *hs = (const f4 *)(a.hs + ((size_t)bh * (a.nseg + 1) + seg + 1) * cells);
         const f4 *gs = (const f4 *)(a.gs + ((size_t)bh * (a.nseg + 1) + seg + 1) * cells);
         for (size_t k = lane; k < cells / 4; k += 64) {
             const f4 p = hs[k], q = gs[k];
             across += (double)p[0] * q[0] + (double)p[1] * q[1] + (double)p[2] * q[2] + (double)p[3] * q[3];
         }
         for (int d = 1; d < 64; d *= 2) across += __shfl_xor(across, d);
-        across *= (double)a.kept[(size_t)bh * a.nseg + seg];
-        const bool in = t < L;
-        float ri = 0.0f, qi = 0.0f, own = 0.0f, dx = 0.0f, raw = 0.0f;
+    }
+    for (int n = nblk - 1; n >= 0; --n) {
+        const int t = t0 + Q * n + r;
+        const bool in = t < L && t < t1;
+        const size_t at = (size_t)bh * a.T + t;
+        float ri = 0.0f, qi = 0.0f, own = 0.0f, dx = 0.0f, raw = 0.0f, delta = 0.0f;
         if (in) {
-            for (int k = 0; k < ntile; ++k) ri += a.rint[k * lines + at], own += a.dlin[k * lines + at];
-            for (int k = 0; k < ptile; ++k) qi += a.qint[k * lines + at], dx += a.xdu[k * lines + at];
-            raw = (float)((const T *)a.dt)[((int64_t)b * a.T + t) * a.dt_row + h] + bias;
+            ri = a.rint[at], own = a.dlin[at], qi = a.qint[at], dx = a.xdu[at];
+            raw = (float)dts[t * a.dt_row] + bias;
+            delta = softplus(raw);
         }
-        float tail = ri, head = __shfl_up(qi, 1, 32);
+        // over the block's lanes (the other half of the wave repeats them where a block is 32)
+        float tail = ri, head = __shfl_up(qi, 1), kept = delta;
         if (r == 0) head = 0.0f;
-#pragma unroll
-        for (int d = 1; d < 32; d *= 2) {
-            const float o = __shfl_down(tail, d, 32), p = __shfl_up(head, d, 32);
-            if (r + d < 32) tail += o;
+        for (int d = 1; d < Q; d *= 2) {
+            const float o = __shfl_down(tail, d), p = __shfl_up(head, d);
+            if (r + d < Q) tail += o;
             if (r >= d) head += p;
+            kept += __shfl_xor(kept, d);
         }
-        if (in && lane < 32) {
+        const float all_r = __shfl(tail, 0), all_q = __shfl(head + qi, Q - 1);
+        across = kept * rate * 1.44269504f < -30.0f ? 0.0 : across - all_q;
+        if (in && lane < Q) {
             const float dl = own + tail + head + (float)across, g = (dx + rate * dl) * sigmoid(raw);
             const float one[1] = {g};
-            store_n<T, 1>(gdt, one);
-            grate = (double)dl * softplus(raw);
-            gbias = (double)g;
+            store_n<T, 1>(gdt + t * a.gdt_row, one);
+            grate += (double)dl * delta;
+            gbias += (double)g;
         }
-        for (int d = 1; d < 32; d *= 2) grate += __shfl_xor(grate, d), gbias += __shfl_xor(gbias, d);
+        across += all_r;
     }
-    if (lane < 32 && t >= L && t < a.T) *gdt = (T)0.0f;
+    for (int t = (used > 0 ? t0 + used : t0) + lane; t < t1; t += 64) gdt[t * a.gdt_row] = (T)0.0f;
+    for (int d = 1; d < 64; d *= 2) grate += __shfl_xor(grate, d), gbias += __shfl_xor(gbias, d);
     if (lane == 0) {
         a.headp[2 * (size_t)blockIdx.x] = grate;
         a.headp[2 * (size_t)blockIdx.x + 1] = gbias;
@@ -103,12 +114,12 @@ __global__ __launch_bounds__(256) void k_ssm_params(SsmArgs a)
     __shared__ double s[3][256];
     const int h = blockIdx.x, tid = threadIdx.x;
     double rate = 0.0, bias = 0.0, skip = 0.0;
-    const int n = a.B * a.nseg, ptile = tiles_of(a.P);
+    const int n = a.B * a.nseg;
     for (int k = tid; k < n; k += 256) {
         const size_t at = ((size_t)(k / a.nseg) * a.H + h) * a.nseg + k % a.nseg;
         rate += a.headp[2 * at];
         bias += a.headp[2 * at + 1];
-        for (int p = 0; p < ptile; ++p) skip += (double)a.skipp[(size_t)p * a.B * a.H * a.nseg + at];
+        skip += (double)a.skipp[at];
     }
     s[0][tid] = rate, s[1][tid] = bias, s[2][tid] = skip;
     for (int d = 128; d > 0; d /= 2) {
@@ -123,22 +134,22 @@ __global__ __launch_bounds__(256) void k_ssm_params(SsmArgs a)
     }
 }
 
-// Gradients of B and C: the sum over the heads that share them.  A thread owns four columns of a row.
+// Gradients of B and C where several workgroups have parts: their sum, in order.  A thread owns four columns of a row.
 template <class T> __global__ __launch_bounds__(256) void k_ssm_heads(SsmArgs a)
 {
-    const int quads = a.N / 4, per = a.H / a.G;
+    const int quads = a.N / 4;
     const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, rows = (int64_t)a.B * a.T;
     if (at >= rows * a.G * quads) return;
-    const int q = (int)(at % quads), grp = (int)(at / quads % a.G);
-    const int64_t row = at / quads / a.G;
+    const int64_t row = at / quads / a.G, col = at % (quads * a.G) * 4;
     const int b = (int)(row / a.T), t = (int)(row % a.T);
     const float *part = blockIdx.y ? a.partc : a.partb;
-    T *out = (T *)(blockIdx.y ? a.gc : a.gb) + row * (blockIdx.y ? a.gc_row : a.gb_row) + grp * a.N + 4 * q;
+    const int chunks = blockIdx.y ? a.c_chunks : a.b_chunks;
+    if (chunks == 1) return;
     f4 s = (f4)0.0f;
     if (t < length_of(a.lengths, b, a.T))
-        for (int h = 0; h < per; ++h) s += *(const f4 *)(part + (row * a.H + grp * per + h) * a.N + 4 * q);
+        for (int k = 0; k < chunks; ++k) s += *(const f4 *)(part + ((int64_t)k * rows + row) * a.G * a.N + col);
     const float o[4] = {s[0], s[1], s[2], s[3]};
-    store_n<T, 4>(out, o);
+    store_n<T, 4>((T *)(blockIdx.y ? a.gc : a.gb) + row * (blockIdx.y ? a.gc_row : a.gb_row) + col, o);
 }
 
 // ---- one more token of each stream --------------------------------------------------------------------------------
@@ -235,7 +246,7 @@ template <class T> __global__ __launch_bounds__(256) void k_ssm_step(StepArgs a)
 // ---- planning -----------------------------------------------------------------------------------------------------
 
 struct SsmPlan {
-    int seg, nseg;
+    int seg, nseg, c_heads, c_chunks, b_heads, b_chunks;
     size_t hs, gs, kept, partc, partb, rint, dlin, qint, xdu, skipp, headp, total;
 };
 
@@ -254,7 +265,20 @@ int make_ssm_plan(int B, int T, int H, int P, int G, int N, bool grad, SsmPlan *
 {
     if (B < 1 || T < 1 || H < 1 || P < 1 || G < 1 || N < 1 || H % G) return SEMICRF_EINVAL;
     if (P % 8 || N % 8 || P > 128 || N > 128 || T > (1 << 30) || (double)B * T * H > 2e9) return SEMICRF_EUNSUPPORTED;
-    p->seg = grad ? BLOCK : segment_length(B, T, H);
+    p->seg = segment_length(B, T, H);
+    p->c_heads = p->b_heads = p->c_chunks = p->b_chunks = 1;
+    if (grad) {
+        // several heads to a workgroup of the gradient kernels where that leaves two for each compute unit
+        const int hpg = H / G;
+        const long groups = (long)B * ((T + 255) / 256) * G;
+        const bool room = P <= 64 && N <= 64 && hpg > 1;
+        p->c_heads = room && groups * ((hpg + 3) / 4) >= 512 ? 4 : 1;
+        p->b_heads = room && groups * ((hpg + 1) / 2) >= 512 ? 2 : 1;
+        p->c_chunks = (hpg + p->c_heads - 1) / p->c_heads;
+        p->b_chunks = (hpg + p->b_heads - 1) / p->b_heads;
+        p->seg = segment_length(B, T, G * p->c_chunks);
+        if (p->seg > 512) p->seg = 512;
+    }
     p->nseg = (T + p->seg - 1) / p->seg;
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -268,24 +292,24 @@ int make_ssm_plan(int B, int T, int H, int P, int G, int N, bool grad, SsmPlan *
     p->kept = take(chain ? bh * p->nseg * 4 : 0);
     if (grad) {
         p->gs = take(bh * (p->nseg + 1) * cells * 4);
-        p->partc = take(rows * H * N * 4);
-        p->partb = take(rows * H * N * 4);
-        p->rint = take(tiles_of(N) * rows * H * 4);
-        p->dlin = take(tiles_of(N) * rows * H * 4);
-        p->qint = take(tiles_of(P) * rows * H * 4);
-        p->xdu = take(tiles_of(P) * rows * H * 4);
-        p->skipp = take(tiles_of(P) * bh * p->nseg * 4);
+        p->partc = take(p->c_chunks > 1 ? p->c_chunks * rows * G * N * 4 : 0);
+        p->partb = take(p->b_chunks > 1 ? p->b_chunks * rows * G * N * 4 : 0);
+        p->rint = take(rows * H * 4);
+        p->dlin = take(rows * H * 4);
+        p->qint = take(rows * H * 4);
+        p->xdu = take(rows * H * 4);
+        p->skipp = take(bh * p->nseg * 4);
         p->headp = take(bh * p->nseg * 16);
     }
     p->total = at;
     return SEMICRF_OK;
 }
 
-int sweep(int type, Use use, bool rev, const SsmArgs &a, hipStream_t st)
+int grad(int type, const SsmArgs &a, hipStream_t st)
 {
-    if (type == ACT_BF16) return ssm_sweep<__bf16>(use, rev, a, st);
-    if (type == ACT_F16) return ssm_sweep<_Float16>(use, rev, a, st);
-    return ssm_sweep<float>(use, rev, a, st);
+    if (type == ACT_BF16) return ssm_grad<__bf16>(a, st);
+    if (type == ACT_F16) return ssm_grad<_Float16>(a, st);
+    return ssm_grad<float>(a, st);
 }
 
 int scan(int type, bool out, bool rev, const SsmArgs &a, hipStream_t st)
@@ -391,23 +415,24 @@ int semicrf_ssm_bwd(const void *x, int64_t x_row, const void *b, int64_t b_row, 
     a.rint = (float *)(w + p.rint); a.dlin = (float *)(w + p.dlin); a.qint = (float *)(w + p.qint);
     a.xdu = (float *)(w + p.xdu); a.skipp = (float *)(w + p.skipp); a.headp = (double *)(w + p.headp);
     const hipStream_t st = (hipStream_t)stream;
-    if (int rc = sweep(type, USE_STATE, false, a, st)) return rc;
-    if (int rc = sweep(type, USE_STATE, true, a, st)) return rc;
+    const int most = P > N ? P : N;
+    a.c_heads = p.c_heads; a.c_chunks = p.c_chunks; a.b_heads = p.b_heads; a.b_chunks = p.b_chunks;
+    a.block = grad_block(type == ACT_F32 ? 3 : type == ACT_F16 ? 2 : 1, most <= 32 ? 32 : most <= 64 ? 64 : 128);
+    if (int rc = scan(type, false, false, a, st)) return rc;
+    if (int rc = scan(type, false, true, a, st)) return rc;
     if (int rc = chain(false, a, st)) return rc;
     if (int rc = chain(true, a, st)) return rc;
-    if (int rc = sweep(type, USE_DC, false, a, st)) return rc;
-    if (int rc = sweep(type, USE_DU, true, a, st)) return rc;
-    if (int rc = sweep(type, USE_DB, true, a, st)) return rc;
+    if (int rc = grad(type, a, st)) return rc;
     const dim3 steps(B * H * p.nseg), heads((unsigned)(((int64_t)B * T * G * (N / 4) + 255) / 256), 2);
     if (type == ACT_BF16) {
         hipLaunchKernelGGL((k_ssm_steps<__bf16>), steps, dim3(64), 0, st, a);
-        hipLaunchKernelGGL((k_ssm_heads<__bf16>), heads, dim3(256), 0, st, a);
+        if (p.b_chunks > 1 || p.c_chunks > 1) hipLaunchKernelGGL((k_ssm_heads<__bf16>), heads, dim3(256), 0, st, a);
     } else if (type == ACT_F16) {
         hipLaunchKernelGGL((k_ssm_steps<_Float16>), steps, dim3(64), 0, st, a);
-        hipLaunchKernelGGL((k_ssm_heads<_Float16>), heads, dim3(256), 0, st, a);
+        if (p.b_chunks > 1 || p.c_chunks > 1) hipLaunchKernelGGL((k_ssm_heads<_Float16>), heads, dim3(256), 0, st, a);
     } else {
         hipLaunchKernelGGL((k_ssm_steps<float>), steps, dim3(64), 0, st, a);
-        hipLaunchKernelGGL((k_ssm_heads<float>), heads, dim3(256), 0, st, a);
+        if (p.b_chunks > 1 || p.c_chunks > 1) hipLaunchKernelGGL((k_ssm_heads<float>), heads, dim3(256), 0, st, a);
     }
     hipLaunchKernelGGL(k_ssm_params, dim3(H), dim3(256), 0, st, a);
     return launched();

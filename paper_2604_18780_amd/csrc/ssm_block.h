@@ -88,6 +88,15 @@ template <class T, int Q, int W, int NT, bool REV> struct Tile {
             o.p[k] = __builtin_shufflevector(*(const bf4 *)(p + k * PART), *(const bf4 *)(q + k * PART), 0, 1, 2, 3, 4, 5, 6, 7);
         return o;
     }
+    // four columns of a row
+    static __device__ __forceinline__ f4 four(const __bf16 *tile, int rw, int at)
+    {
+        const __bf16 *p = tile + cell(rw, at);
+        f4 v = __builtin_convertvector(*(const bf4 *)(p + (RAW - 1) * PART), f4);
+#pragma unroll
+        for (int k = RAW - 2; k >= 0; --k) v += __builtin_convertvector(*(const bf4 *)(p + k * PART), f4);
+        return v;
+    }
     // inner index = row: rows first + 4g.., first + 16 + 4g.. of column at + lane % 16
     static __device__ __forceinline__ Op<RAW> by_col(const __bf16 *tile, int first, int at, int lane)
     {
@@ -185,18 +194,19 @@ template <int Q, bool REV> __device__ __forceinline__ void make_steps(Steps<Q> &
     }
 }
 
-// Scores of a block: sixteen queries `it`, sixteen keys `jt` <= it, as four keys of one query in a lane.  Where the two are the
-// same sixteen, only the last of a lane's keys takes a power; the earlier ones multiply what is kept on the way to it.
-template <int Q> __device__ __forceinline__ f4 weigh(const Steps<Q> &s, f4 m, int it, int jt, int i16, int g)
+// Weights of scores: sixteen queries `it`, sixteen keys `jt` <= it, as four keys of one query in a lane; 0 where the key lies
+// behind the query.  Where the two are the same sixteen, only the last of a lane's keys takes a power; the earlier ones
+// multiply what is kept on the way to it.
+template <int Q> __device__ __forceinline__ f4 weights(const Steps<Q> &s, int it, int jt, int i16, int g)
 {
-    if (jt < it) return m * *(const f4 *)(s.from[it - 1] + 16 * jt + 4 * g) * s.query[16 * it + i16];
+    if (jt < it) return *(const f4 *)(s.from[it - 1] + 16 * jt + 4 * g) * s.query[16 * it + i16];
     const f4 key = *(const f4 *)(s.key + 16 * it + 4 * g), step = *(const f4 *)(s.step + 16 * it + 4 * g);
     const float last = fminf((float)(s.c[16 * it + i16] - s.c[16 * it + 4 * g + 3]), 0.0f);
     f4 e;
     e[3] = i16 >= 4 * g + 3 ? __builtin_amdgcn_exp2f(last) : 0.0f;
 #pragma unroll
     for (int r = 2; r >= 0; --r) e[r] = i16 == 4 * g + r ? 1.0f : e[r + 1] * step[r + 1];
-    return m * (e * key);
+    return e * key;
 }
 
 // Where scores are handed from the wave that makes them to those that multiply with them: operands of queries 16 it.., keys
@@ -230,6 +240,38 @@ template <int Q, int MADE> struct Scores {
         return o;
     }
 };
+
+// Sums over a row of sixteen lanes, and over the four rows of a wave.
+template <int CTRL> __device__ __forceinline__ float moved(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float sum16(float v)  // in every lane
+{
+    v += moved<0x128>(v);  // rotated by 8, 4, 2, 1
+    v += moved<0x124>(v);
+    v += moved<0x122>(v);
+    return v + moved<0x121>(v);
+}
+__device__ __forceinline__ float prefix16(float v)
+{
+    v += moved<0x111>(v);
+    v += moved<0x112>(v);
+    v += moved<0x114>(v);
+    return v + moved<0x118>(v);
+}
+__device__ __forceinline__ float suffix16(float v)
+{
+    v += moved<0x101>(v);
+    v += moved<0x102>(v);
+    v += moved<0x104>(v);
+    return v + moved<0x108>(v);
+}
+__device__ __forceinline__ float sum_rows(float v)
+{
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
 
 __device__ __forceinline__ void lds_barrier()
 {

@@ -108,7 +108,7 @@ template <class T, int Q, int DK, int PV, bool OUT, bool REV> __global__ __launc
                 f4 m = (f4)0.0f;
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) m = mma(m, TK::by_row(sk, 16 * jt + i16, 32 * ks, g), q[it][ks]);
-                m = weigh(s, m, it, jt, i16, g);
+                m *= weights(s, it, jt, i16, g);
                 if (it == jt) m += skips;
                 SC::put(sm, it, jt, m, lane);
             }
