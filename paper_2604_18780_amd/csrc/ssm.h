@@ -27,8 +27,7 @@ struct SsmArgs {
     const float *grad_last;   // [B,H,P,N] or null: gradient of the state after the last token
     int B, T, H, P, G, N;
     int seg, nseg;            // positions of a segment (a multiple of 64) and how many there are
-    int c_heads, c_chunks;    // heads of a group that a workgroup of k_ssm_grad_c takes, and how many such there are
-    int b_heads, b_chunks;    // of k_ssm_grad_xb
+    int heads, chunks;        // heads of a group that a workgroup of the gradient kernels takes, and how many such there are
     int block;                // positions of a block of the gradient kernels
     void *y;
     int64_t y_row;
@@ -45,8 +44,13 @@ struct SsmArgs {
     double *headp;            // [B*H*nseg][2] sums for rate and bias
 };
 
-// Positions of a block of the gradient kernels: what their four staged operands (of `raw` parts, `dim` wide) leave room for.
-constexpr int grad_block(int raw, int dim) { return raw * dim <= 64 ? 64 : 32; }
+// Positions of a block of the gradient kernels, by the parts and the width of their four staged operands.  Blocks of 64 read a
+// state half as often, but want 250 registers, two waves to a SIMD, where blocks of 32 run three: 4 x 100 000 tokens, 8 heads of 64,
+// 64 states, bfloat16 took 611 + 1053 us with blocks of 64 and takes 485 + 627.
+// Heads that a workgroup of the gradient kernels takes where B and C are shared: one needs fewer registers, but leaves a part of the
+// gradients of B and C for each head (694 + 451 us and 331 to sum the parts, against 627 + 485 and 176), four spill.
+constexpr int GRAD_HEADS = 2;
+constexpr int grad_block(int raw, int dim) { return raw * dim <= 32 ? 64 : 32; }
 
 // one instantiation per storage type, each in a translation unit of its own
 template <class T> int ssm_scan(bool out, bool rev, const SsmArgs &a, hipStream_t st);

@@ -143,11 +143,9 @@ template <class T> __global__ __launch_bounds__(256) void k_ssm_heads(SsmArgs a)
     const int64_t row = at / quads / a.G, col = at % (quads * a.G) * 4;
     const int b = (int)(row / a.T), t = (int)(row % a.T);
     const float *part = blockIdx.y ? a.partc : a.partb;
-    const int chunks = blockIdx.y ? a.c_chunks : a.b_chunks;
-    if (chunks == 1) return;
     f4 s = (f4)0.0f;
     if (t < length_of(a.lengths, b, a.T))
-        for (int k = 0; k < chunks; ++k) s += *(const f4 *)(part + ((int64_t)k * rows + row) * a.G * a.N + col);
+        for (int k = 0; k < a.chunks; ++k) s += *(const f4 *)(part + ((int64_t)k * rows + row) * a.G * a.N + col);
     const float o[4] = {s[0], s[1], s[2], s[3]};
     store_n<T, 4>((T *)(blockIdx.y ? a.gc : a.gb) + row * (blockIdx.y ? a.gc_row : a.gb_row) + col, o);
 }
@@ -246,7 +244,7 @@ template <class T> __global__ __launch_bounds__(256) void k_ssm_step(StepArgs a)
 // ---- planning -----------------------------------------------------------------------------------------------------
 
 struct SsmPlan {
-    int seg, nseg, c_heads, c_chunks, b_heads, b_chunks;
+    int seg, nseg, heads, chunks;
     size_t hs, gs, kept, partc, partb, rint, dlin, qint, xdu, skipp, headp, total;
 };
 
@@ -266,17 +264,15 @@ int make_ssm_plan(int B, int T, int H, int P, int G, int N, bool grad, SsmPlan *
     if (B < 1 || T < 1 || H < 1 || P < 1 || G < 1 || N < 1 || H % G) return SEMICRF_EINVAL;
     if (P % 8 || N % 8 || P > 128 || N > 128 || T > (1 << 30) || (double)B * T * H > 2e9) return SEMICRF_EUNSUPPORTED;
     p->seg = segment_length(B, T, H);
-    p->c_heads = p->b_heads = p->c_chunks = p->b_chunks = 1;
+    p->heads = p->chunks = 1;
     if (grad) {
-        // several heads to a workgroup of the gradient kernels where that leaves two for each compute unit
+        // two heads to a workgroup of the gradient kernels where that leaves two workgroups for each compute unit
         const int hpg = H / G;
         const long groups = (long)B * ((T + 255) / 256) * G;
         const bool room = P <= 64 && N <= 64 && hpg > 1;
-        p->c_heads = room && groups * ((hpg + 3) / 4) >= 512 ? 4 : 1;
-        p->b_heads = room && groups * ((hpg + 1) / 2) >= 512 ? 2 : 1;
-        p->c_chunks = (hpg + p->c_heads - 1) / p->c_heads;
-        p->b_chunks = (hpg + p->b_heads - 1) / p->b_heads;
-        p->seg = segment_length(B, T, G * p->c_chunks);
+        p->heads = room && groups * ((hpg + GRAD_HEADS - 1) / GRAD_HEADS) >= 512 ? GRAD_HEADS : 1;
+        p->chunks = (hpg + p->heads - 1) / p->heads;
+        p->seg = segment_length(B, T, G * p->chunks);
         if (p->seg > 512) p->seg = 512;
     }
     p->nseg = (T + p->seg - 1) / p->seg;
@@ -292,8 +288,8 @@ int make_ssm_plan(int B, int T, int H, int P, int G, int N, bool grad, SsmPlan *
     p->kept = take(chain ? bh * p->nseg * 4 : 0);
     if (grad) {
         p->gs = take(bh * (p->nseg + 1) * cells * 4);
-        p->partc = take(p->c_chunks > 1 ? p->c_chunks * rows * G * N * 4 : 0);
-        p->partb = take(p->b_chunks > 1 ? p->b_chunks * rows * G * N * 4 : 0);
+        p->partc = take(p->chunks > 1 ? p->chunks * rows * G * N * 4 : 0);
+        p->partb = take(p->chunks > 1 ? p->chunks * rows * G * N * 4 : 0);
         p->rint = take(rows * H * 4);
         p->dlin = take(rows * H * 4);
         p->qint = take(rows * H * 4);
@@ -416,7 +412,7 @@ int semicrf_ssm_bwd(const void *x, int64_t x_row, const void *b, int64_t b_row, 
     a.xdu = (float *)(w + p.xdu); a.skipp = (float *)(w + p.skipp); a.headp = (double *)(w + p.headp);
     const hipStream_t st = (hipStream_t)stream;
     const int most = P > N ? P : N;
-    a.c_heads = p.c_heads; a.c_chunks = p.c_chunks; a.b_heads = p.b_heads; a.b_chunks = p.b_chunks;
+    a.heads = p.heads; a.chunks = p.chunks;
     a.block = grad_block(type == ACT_F32 ? 3 : type == ACT_F16 ? 2 : 1, most <= 32 ? 32 : most <= 64 ? 64 : 128);
     if (int rc = scan(type, false, false, a, st)) return rc;
     if (int rc = scan(type, false, true, a, st)) return rc;
@@ -426,13 +422,13 @@ int semicrf_ssm_bwd(const void *x, int64_t x_row, const void *b, int64_t b_row, 
     const dim3 steps(B * H * p.nseg), heads((unsigned)(((int64_t)B * T * G * (N / 4) + 255) / 256), 2);
     if (type == ACT_BF16) {
         hipLaunchKernelGGL((k_ssm_steps<__bf16>), steps, dim3(64), 0, st, a);
-        if (p.b_chunks > 1 || p.c_chunks > 1) hipLaunchKernelGGL((k_ssm_heads<__bf16>), heads, dim3(256), 0, st, a);
+        if (p.chunks > 1) hipLaunchKernelGGL((k_ssm_heads<__bf16>), heads, dim3(256), 0, st, a);
     } else if (type == ACT_F16) {
         hipLaunchKernelGGL((k_ssm_steps<_Float16>), steps, dim3(64), 0, st, a);
-        if (p.b_chunks > 1 || p.c_chunks > 1) hipLaunchKernelGGL((k_ssm_heads<_Float16>), heads, dim3(256), 0, st, a);
+        if (p.chunks > 1) hipLaunchKernelGGL((k_ssm_heads<_Float16>), heads, dim3(256), 0, st, a);
     } else {
         hipLaunchKernelGGL((k_ssm_steps<float>), steps, dim3(64), 0, st, a);
-        if (p.b_chunks > 1 || p.c_chunks > 1) hipLaunchKernelGGL((k_ssm_heads<float>), heads, dim3(256), 0, st, a);
+        if (p.chunks > 1) hipLaunchKernelGGL((k_ssm_heads<float>), heads, dim3(256), 0, st, a);
     }
     hipLaunchKernelGGL(k_ssm_params, dim3(H), dim3(256), 0, st, a);
     return launched();

@@ -6,13 +6,45 @@
 
 namespace semicrf_enc {
 
-// Rows of one sequence behind a range check: what lies beyond `bytes` reads as zeros and is not written.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const void *base, int64_t bytes)
+// Rows of one sequence behind a range check: of the Q rows from `first`, `bytes` apart, those from the `left`-th on read as zeros
+// and are not written.  An offset that a scalar adds (a head's columns) counts in the range, as it does within a row.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const void *first, int left, int Q, int bytes)
 {
-    const int n = bytes < 0 ? 0 : bytes > 0x7ffffff0 ? 0x7ffffff0 : (int)bytes;
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, n, 0x00020000);
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(first), 0, left >= Q ? 0x7ffffff0 : left > 0 ? left * bytes : 0, 0x00020000);
 }
 constexpr uint32_t OUTSIDE = 0x80000000u;  // an offset beyond any range
+
+// Four columns of a row to memory, by range: `off` is the lane's, in bytes, from the rows' first.
+template <class T> __device__ __forceinline__ void store_four(__amdgpu_buffer_rsrc_t rows, uint32_t off, int from_row, f4 v)
+{
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    const T4 o = __builtin_convertvector(v, T4);
+    if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, o), rows, (int)off, from_row, 0);
+    else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u2, o), rows, (int)off, from_row, 0);
+}
+
+// dt of a block's positions, one a lane.  The raw value is kept until it is used: a load that is converted at once waits for
+// every load before it.
+template <class T> struct Dt {
+    uint32_t raw;
+    bool in;
+    // row r of the block whose rows at the head's column begin at `first`, `bytes` apart; `left` positions exist
+    __device__ __forceinline__ void fetch(const char *first, int bytes, int r, int left)
+    {
+        in = r < left;
+        const __amdgpu_buffer_rsrc_t from = rows_at(first, left > 0 ? 64 : 0, 64, bytes);
+        const int off = in ? r * bytes : (int)OUTSIDE;
+        if constexpr (sizeof(T) == 4) raw = __builtin_amdgcn_raw_buffer_load_b32(from, off, 0, 0);
+        else raw = (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(from, off, 0, 0);
+    }
+    __device__ __forceinline__ float value() const
+    {
+        float v;
+        if constexpr (sizeof(T) == 4) v = __builtin_bit_cast(float, raw);
+        else v = (float)__builtin_bit_cast(T, (uint16_t)raw);
+        return in ? v : -INFINITY;
+    }
+};
 
 // One operand's rows of a block: Q rows of `dim` elements, staged as bfloat16 parts W wide (padding columns zeros), by NT
 // threads.  REV: row r is the block's position Q-1-r.
@@ -21,8 +53,6 @@ constexpr uint32_t OUTSIDE = 0x80000000u;  // an offset beyond any range
 template <class T, int Q, int W, int NT, bool REV> struct Tile {
     static constexpr int RAW = Parts<T>::raw, E = PER16<T>, PART = Q * W, ELEMS = RAW * PART;
     static constexpr int PR = W / E, ALL = Q * PR, CH = (ALL + NT - 1) / NT;
-    const T *base;   // the sequence's first row, at the head's or group's columns
-    int64_t row;
     uint32_t off[CH];
     u4 r[CH];
     static __device__ __forceinline__ int mix(int rw)
@@ -32,41 +62,49 @@ template <class T, int Q, int W, int NT, bool REV> struct Tile {
     }
     // element `col` (a multiple of 4) of row rw
     static __device__ __forceinline__ int cell(int rw, int col) { return rw * W + (((col >> 2) ^ mix(rw)) << 2); }
-    __device__ __forceinline__ void init(const T *b, int64_t rw, int dim, int tid)
+    // rows `bytes` apart
+    __device__ __forceinline__ void init(int bytes, int dim, int tid)
     {
-        base = b;
-        row = rw;
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             const int at = tid + NT * i, k = at / PR, col = at % PR * E;
-            off[i] = k < Q && col < dim ? (uint32_t)((REV ? Q - 1 - k : k) * row + col) * (uint32_t)sizeof(T) : OUTSIDE;
+            off[i] = k < Q && col < dim ? (uint32_t)((REV ? Q - 1 - k : k) * bytes + col * (int)sizeof(T)) : OUTSIDE;
         }
     }
-    __device__ __forceinline__ void fetch(int t, int L)
+    __device__ __forceinline__ void fetch(__amdgpu_buffer_rsrc_t rows, int columns)
     {
-        const __amdgpu_buffer_rsrc_t rows = rows_from(base + t * row, (L - t) * row * (int64_t)sizeof(T));
 #pragma unroll
-        for (int i = 0; i < CH; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b128(rows, (int)off[i], 0, 0);
+        for (int i = 0; i < CH; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b128(rows, (int)off[i], columns, 0);
     }
-    __device__ __forceinline__ void put(__bf16 *tile, int tid) const
+    // where this thread's chunks lie in a tile: the same for all operands of one shape
+    struct Place {
+        int a[CH], b[CH];
+        __device__ __forceinline__ Place(int tid)
+        {
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const int at = tid + NT * i, k = at / PR % Q, col = at % PR * E;
+                a[i] = cell(k, col);
+                b[i] = E == 8 ? cell(k, col + 4) : 0;
+            }
+        }
+    };
+    __device__ __forceinline__ void put(__bf16 *tile, const Place &to, int tid) const
     {
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            const int at = tid + NT * i, k = at / PR, col = at % PR * E;
-            if (ALL % NT != 0 && at >= ALL) break;
-            __bf16 *to = tile + cell(k, col);
+            if (ALL % NT != 0 && tid + NT * i >= ALL) break;
             if constexpr (RAW == 1) {
-                *(u2 *)to = (u2){r[i][0], r[i][1]};
-                *(u2 *)(tile + cell(k, col + 4)) = (u2){r[i][2], r[i][3]};
+                *(u2 *)(tile + to.a[i]) = (u2){r[i][0], r[i][1]};
+                *(u2 *)(tile + to.b[i]) = (u2){r[i][2], r[i][3]};
             } else if constexpr (RAW == 2) {
                 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
                 const Op<2> o = split<2>(__builtin_convertvector(__builtin_bit_cast(h8, r[i]), f8));
-                __bf16 *next = tile + cell(k, col + 4);
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const u4 v = __builtin_bit_cast(u4, o.p[j]);
-                    *(u2 *)(to + j * PART) = (u2){v[0], v[1]};
-                    *(u2 *)(next + j * PART) = (u2){v[2], v[3]};
+                    *(u2 *)(tile + to.a[i] + j * PART) = (u2){v[0], v[1]};
+                    *(u2 *)(tile + to.b[i] + j * PART) = (u2){v[2], v[3]};
                 }
             } else {
                 const f4 v = __builtin_bit_cast(f4, r[i]);
@@ -74,43 +112,65 @@ template <class T, int Q, int W, int NT, bool REV> struct Tile {
                 uint32_t p[3][2];
                 split_pairs<3, 2>(x, p);
 #pragma unroll
-                for (int j = 0; j < 3; ++j) *(u2 *)(to + j * PART) = (u2){p[j][0], p[j][1]};
+                for (int j = 0; j < 3; ++j) *(u2 *)(tile + to.a[i] + j * PART) = (u2){p[j][0], p[j][1]};
             }
         }
     }
-    // inner index = column: columns at + 4g.., at + 16 + 4g.. of a row
-    static __device__ __forceinline__ Op<RAW> by_row(const __bf16 *tile, int rw, int at, int g)
+    // Where a lane reads.  Of a cell's number the mix changes its low four bits (three where a row is 32 wide), so the places of
+    // all operands of a tile are four (two) numbers of the lane's and constants: the reads' own offsets.
+    struct Lane {
+        int row[4], col[4];  // of row lane % 16 / of row lane / 4: by bits 2 and 3 of the cell
+        int own, four;       // columns 16 w..: read transposed; four of row lane % 16
+        __device__ __forceinline__ Lane(int lane, int w)
+        {
+            const int g = lane >> 4, i16 = lane & 15;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                row[k] = cell(i16, W >= 64 ? 16 * k + 4 * g : 16 * (k & 1) + 4 * g);
+                col[k] = cell(lane >> 2, W >= 64 ? 16 * k + 4 * (lane & 3) : 16 * (k & 1) % W + 4 * (lane & 3));
+            }
+            own = cell(lane >> 2, 16 * w + 4 * (lane & 3));
+            four = cell(i16, 16 * w + 4 * g);
+        }
+    };
+    // inner index = column: columns 32 ks + 4g.., + 16 + 4g.. of rows 16 it + lane % 16
+    static __device__ __forceinline__ Op<RAW> by_row(const __bf16 *tile, const Lane &at, int it, int ks)
     {
         Op<RAW> o;
-        const __bf16 *p = tile + cell(rw, at + 4 * g), *q = tile + cell(rw, at + 16 + 4 * g);
+        const int more = 16 * it * W + ks / 2 * 64, k0 = W >= 64 ? ks % 2 * 2 : 0;
 #pragma unroll
         for (int k = 0; k < RAW; ++k)
-            o.p[k] = __builtin_shufflevector(*(const bf4 *)(p + k * PART), *(const bf4 *)(q + k * PART), 0, 1, 2, 3, 4, 5, 6, 7);
+            o.p[k] = __builtin_shufflevector(*(const bf4 *)(tile + at.row[k0] + (more + k * PART)),
+                                             *(const bf4 *)(tile + at.row[k0 + 1] + (more + k * PART)), 0, 1, 2, 3, 4, 5, 6, 7);
         return o;
     }
-    // four columns of a row
-    static __device__ __forceinline__ f4 four(const __bf16 *tile, int rw, int at)
+    template <int n> static __device__ __forceinline__ Op<n> transposed(const __bf16 *tile, int from, int more, int part)
     {
-        const __bf16 *p = tile + cell(rw, at);
+        typedef __attribute__((address_space(3))) s4 *lds;
+        Op<n> o;
+        __bf16 *p = const_cast<__bf16 *>(tile) + from;
+#pragma unroll
+        for (int k = 0; k < n; ++k) {
+            const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(p + (more + k * part)));
+            const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(p + (more + k * part + 16 * W)));
+            o.p[k] = __builtin_shufflevector(__builtin_bit_cast(bf4, lo), __builtin_bit_cast(bf4, hi), 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+        return o;
+    }
+    // inner index = row: rows 32 ks + 4g.., + 16 + 4g.. of column 16 kt + lane % 16 / of the wave's own sixteen columns
+    static __device__ __forceinline__ Op<RAW> by_col(const __bf16 *tile, const Lane &at, int ks, int kt)
+    {
+        return transposed<RAW>(tile, at.col[W >= 64 ? kt % 4 : kt], 32 * ks * W + (W >= 64 ? kt / 4 * 64 : 0), PART);
+    }
+    static __device__ __forceinline__ Op<RAW> own_col(const __bf16 *tile, const Lane &at, int ks) { return transposed<RAW>(tile, at.own, 32 * ks * W, PART); }
+    // columns 16 w + 4g.. of row 16 it + lane % 16
+    static __device__ __forceinline__ f4 four(const __bf16 *tile, const Lane &at, int it)
+    {
+        const __bf16 *p = tile + at.four + 16 * it * W;
         f4 v = __builtin_convertvector(*(const bf4 *)(p + (RAW - 1) * PART), f4);
 #pragma unroll
         for (int k = RAW - 2; k >= 0; --k) v += __builtin_convertvector(*(const bf4 *)(p + k * PART), f4);
         return v;
-    }
-    // inner index = row: rows first + 4g.., first + 16 + 4g.. of column at + lane % 16
-    static __device__ __forceinline__ Op<RAW> by_col(const __bf16 *tile, int first, int at, int lane)
-    {
-        typedef __attribute__((address_space(3))) s4 *lds;
-        Op<RAW> o;
-        // rows sixteen apart are mixed alike
-        __bf16 *p = const_cast<__bf16 *>(tile) + cell(first + (lane >> 2), at + 4 * (lane & 3));
-#pragma unroll
-        for (int k = 0; k < RAW; ++k) {
-            const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(p + k * PART));
-            const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(p + k * PART + 16 * W));
-            o.p[k] = __builtin_shufflevector(__builtin_bit_cast(bf4, lo), __builtin_bit_cast(bf4, hi), 0, 1, 2, 3, 4, 5, 6, 7);
-        }
-        return o;
     }
 };
 
@@ -269,8 +329,15 @@ __device__ __forceinline__ float suffix16(float v)
 }
 __device__ __forceinline__ float sum_rows(float v)
 {
-    v += __shfl_xor(v, 16);
-    return v + __shfl_xor(v, 32);
+    // the two operands of a swap have to be two registers, or the compiler takes its two results for one
+    uint32_t x = __builtin_bit_cast(uint32_t, v), y = x;
+    asm("" : "+v"(y));
+    const auto a = __builtin_amdgcn_permlane16_swap(x, y, false, false);
+    x = __builtin_bit_cast(uint32_t, __builtin_bit_cast(float, (uint32_t)a[0]) + __builtin_bit_cast(float, (uint32_t)a[1]));
+    y = x;
+    asm("" : "+v"(y));
+    const auto b = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+    return __builtin_bit_cast(float, (uint32_t)b[0]) + __builtin_bit_cast(float, (uint32_t)b[1]);
 }
 
 __device__ __forceinline__ void lds_barrier()

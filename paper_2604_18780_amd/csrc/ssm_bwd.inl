@@ -18,6 +18,9 @@
 
 namespace semicrf_enc {
 
+// Waves to a SIMD that the registers are cut for.
+constexpr int waves_for(int raw, int Q, int DM) { return Q == 32 && DM <= 64 && raw == 1 ? 3 : 2; }
+
 // What both kernels know of their workgroup.
 template <class T> struct Place {
     int b, seg, grp, chunk, h0, nh, L, t0, t1, nblk;
@@ -44,16 +47,56 @@ template <class T> struct Place {
     }
 };
 
-// Four columns of sixteen positions of a lane to a row of the gradient of B or C: at once in its type where one workgroup sums
-// all heads, else to the workgroup's part.
-template <class T> __device__ __forceinline__ void store_shared(const SsmArgs &a, void *out, int64_t out_row, float *part, const Place<T> &w,
-                                                                int chunks, int t, int n, f4 v)
+// Rows of the gradient of B or C: in its type where one workgroup sums all heads, else the workgroup's part.
+template <class T> struct SharedOut {
+    char *first;
+    int row;  // bytes
+    bool whole;
+    __device__ __forceinline__ SharedOut(const SsmArgs &a, void *out, int64_t out_row, float *part, int chunks, const Place<T> &w)
+    {
+        whole = chunks == 1;
+        row = whole ? (int)(out_row * (int64_t)sizeof(T)) : a.G * a.N * 4;
+        first = whole ? (char *)((T *)out + w.rb * out_row + w.grp * a.N)
+                      : (char *)(part + (((size_t)w.chunk * a.B * a.T + w.rb) * a.G + w.grp) * a.N);
+    }
+    // row r of a block from position `base`, `above` rows further down; columns n.. of N
+    template <int Q> __device__ __forceinline__ void put(int base, int r, int above, int n, int N, int t1, f4 v) const
+    {
+        const __amdgpu_buffer_rsrc_t rows = rows_at(first + (int64_t)base * row, t1 - base, Q, row);
+        const uint32_t off = n < N ? (uint32_t)(r * row + n * (whole ? (int)sizeof(T) : 4)) : OUTSIDE;
+        if (whole) store_four<T>(rows, off, above * row, v);
+        else store_four<float>(rows, off, above * row, v);
+    }
+};
+
+// A value for position base + r of a head's line, r >= 0.  Stores are never skipped by a branch, here and below: the wait for the
+// rows that are on their way could not tell how many stores came after them, and would wait for all.
+template <int Q> __device__ __forceinline__ void put_line(float *line, int base, int t1, int r, float v)
 {
-    if (t >= w.t1 || n >= a.N) return;
-    const float o[4] = {v[0], v[1], v[2], v[3]};
-    if (chunks == 1) store_n<T, 4>((T *)out + (w.rb + t) * out_row + w.grp * a.N + n, o);
-    else store_n<float, 4>(part + (((size_t)w.chunk * a.B * a.T + w.rb + t) * a.G + w.grp) * a.N + n, o);
+    __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), rows_at(line + base, t1 - base, Q, 4), r >= 0 ? 4 * r : (int)OUTSIDE, 0, 0);
 }
+
+// The operands' rows: where the block that is fetched next begins, at the first head's (the group's) columns.
+template <class T> struct Sources {
+    const char *x, *y, *b, *c, *dt;
+    int x_bytes, y_bytes, b_bytes, c_bytes, dt_bytes;
+    __device__ __forceinline__ Sources(const SsmArgs &a, const Place<T> &w, int64_t first)
+    {
+        constexpr int e = (int)sizeof(T);
+        x_bytes = (int)a.x_row * e, y_bytes = (int)a.gy_row * e, b_bytes = (int)a.b_row * e, c_bytes = (int)a.c_row * e;
+        dt_bytes = (int)a.dt_row * e;
+        const int64_t at = w.rb + first;
+        x = (const char *)a.x + at * x_bytes + w.h0 * a.P * e;
+        y = (const char *)a.gy + at * y_bytes + w.h0 * a.P * e;
+        b = (const char *)a.b + at * b_bytes + w.grp * a.N * e;
+        c = (const char *)a.c + at * c_bytes + w.grp * a.N * e;
+        dt = (const char *)a.dt + at * dt_bytes + w.h0 * e;
+    }
+    __device__ __forceinline__ void move(int rows)
+    {
+        x += (int64_t)rows * x_bytes, y += (int64_t)rows * y_bytes, b += (int64_t)rows * b_bytes, c += (int64_t)rows * c_bytes;
+    }
+};
 
 // Zeros in the rows [first, t1) of `width` columns.
 template <class T> __device__ __forceinline__ void clear_rows(T *out, int64_t row, int first, int t1, int width, int tid, int nt)
@@ -65,77 +108,78 @@ template <class T> __device__ __forceinline__ void clear_rows(T *out, int64_t ro
 
 // ---- gradient of C ------------------------------------------------------------------------------------------------
 //   dC_i = sum_h sum_{j<=i} e^{c_i-c_j} (dy_i . u_j) B_j:  queries dy, keys x (scaled by delta), values B; state H [P x N]
-template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, 2) void k_ssm_grad_c(SsmArgs a)
+template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, waves_for(Parts<T>::raw, Q, DM)) void k_ssm_grad_c(SsmArgs a)
 {
     constexpr int NT = DM * 4, NW = DM / 16, KT = DM / 16, KS = DM / 32, IT = Q / 16, QS = Q / 32;
-    constexpr int RAW = Parts<T>::raw, MADE = Parts<T>::made, HELD = 3;
+    constexpr int RAW = Parts<T>::raw, MADE = Parts<T>::made, HELD = 3, E = (int)sizeof(T);
     typedef Tile<T, Q, DM, NT, false> TL;
     typedef Scores<Q, MADE> SC;
     constexpr int OWN = (SC::TILES + NW - 1) / NW;  // tiles of scores a wave makes at most
-    __shared__ __attribute__((aligned(16))) __bf16 sx[TL::ELEMS];
-    __shared__ __attribute__((aligned(16))) __bf16 sy[TL::ELEMS];
-    __shared__ __attribute__((aligned(16))) __bf16 sb[TL::ELEMS];
-    __shared__ __attribute__((aligned(16))) __bf16 sc[TL::ELEMS];
-    __shared__ __attribute__((aligned(16))) __bf16 sm[SC::ELEMS];
-    __shared__ __attribute__((aligned(16))) Steps<Q> ss[HB];
+    constexpr int TURNS = (IT + NW - 1) / NW;       // sixteens of positions whose sums a wave makes
+    // one array, so that operands' places differ by constants
+    __shared__ __attribute__((aligned(16))) __bf16 pool[4 * TL::ELEMS + SC::ELEMS];
+    __bf16 *const sx = pool, *const sy = sx + TL::ELEMS, *const sb = sy + TL::ELEMS, *const sc = sb + TL::ELEMS, *const sm = sc + TL::ELEMS;
+    __shared__ __attribute__((aligned(16))) Steps<Q> ss[2][HB];
     __shared__ float rp[NW][Q];             // by wave: its columns' part of rint
     __shared__ float ends[SC::TILES][16];   // sums of a tile of W by its later positions (on the diagonal: dlin), ..
     __shared__ float starts[SC::TILES][16]; // .. and by its earlier ones
 
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, i16 = lane & 15;
-    const Place<T> at(a, HB, Q, a.c_chunks);
+    const Place<T> at(a, HB, Q, a.chunks);
     if (!at.any) return;
     const size_t cells = (size_t)a.P * a.N;
     const int n0 = 16 * w + i16;  // this lane's column of the state
 
+    Sources<T> src(a, at, at.t0);
     TL rx, ry, rbt, rct;
-    rbt.init((const T *)a.b + at.rb * a.b_row + at.grp * a.N, a.b_row, a.N, tid);
-    rct.init((const T *)a.c + at.rb * a.c_row + at.grp * a.N, a.c_row, a.N, tid);
-    const T *x0 = (const T *)a.x + at.rb * a.x_row, *y0 = (const T *)a.gy + at.rb * a.gy_row;
-    rx.init(x0 + at.h0 * a.P, a.x_row, a.P, tid);
-    ry.init(y0 + at.h0 * a.P, a.gy_row, a.P, tid);
+    const typename TL::Lane ln(lane, w);
+    const typename TL::Place pl(tid);
+    rx.init(src.x_bytes, a.P, tid);
+    ry.init(src.y_bytes, a.P, tid);
+    rbt.init(src.b_bytes, a.N, tid);
+    rct.init(src.c_bytes, a.N, tid);
 
     f4 S[HB][KT];
+    float rate[HB], bias[HB];
 #pragma unroll
     for (int k = 0; k < HB; ++k) {
-        const float *from = a.hs + ((size_t)(at.b * a.H + at.h0 + k) * (a.nseg + 1) + at.seg) * cells;
+        const int head = k < at.nh ? at.h0 + k : at.h0;
+        rate[k] = a.rate[head];
+        bias[k] = a.dt_bias ? a.dt_bias[head] : 0.0f;
+        const float *from = a.hs + ((size_t)(at.b * a.H + head) * (a.nseg + 1) + at.seg) * cells;
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
             S[k][kt] = (f4)0.0f;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int p = 16 * kt + 4 * g + r;
-                if (k < at.nh && at.nblk && p < a.P && n0 < a.N) S[k][kt][r] = from[(size_t)p * a.N + n0];
+                if (at.nblk && p < a.P && n0 < a.N) S[k][kt][r] = from[(size_t)p * a.N + n0];
             }
         }
     }
-    // steps: wave w makes those of heads w, w + NW, ..
-    constexpr int MINE = (HB + NW - 1) / NW;
-    float dt_next[MINE];
-    auto fetch_dt = [&](int n) {
-#pragma unroll
-        for (int k = 0; k < MINE; ++k) {
-            const int head = w + NW * k, t = at.t0 + Q * n + lane % Q;
-            dt_next[k] = head < at.nh && n < at.nblk && t < at.L ? (float)((const T *)a.dt)[(at.rb + t) * a.dt_row + at.h0 + head] : -INFINITY;
-        }
+    // Steps are made a block ahead, by the last wave, which has the fewest scores to make; dt comes another block ahead.
+    Dt<T> dt[HB];
+    auto fetch_dt = [&](int n, int k) {
+        dt[k].fetch(src.dt + (int64_t)Q * n * src.dt_bytes + (k < at.nh ? k * E : 0), src.dt_bytes, lane % Q, n < at.nblk ? at.L - at.t0 - Q * n : 0);
     };
-    fetch_dt(0);
     if (at.nblk) {
-        rbt.fetch(at.t0, at.L);
-        rct.fetch(at.t0, at.L);
-        rx.fetch(at.t0, at.L);
-        ry.fetch(at.t0, at.L);
+        rbt.fetch(rows_at(src.b, at.L - at.t0, Q, src.b_bytes), 0);
+        rct.fetch(rows_at(src.c, at.L - at.t0, Q, src.c_bytes), 0);
+        rx.fetch(rows_at(src.x, at.L - at.t0, Q, src.x_bytes), 0);
+        ry.fetch(rows_at(src.y, at.L - at.t0, Q, src.y_bytes), 0);
         SC::clear(sm, tid, NT);
+#pragma unroll
+        for (int k = 0; k < HB; ++k) {
+            fetch_dt(0, k);
+            if (w == k % NW) make_steps<Q, false>(ss[0][k], dt[k].value(), bias[k], rate[k], true, lane);
+            fetch_dt(1, k);
+        }
     }
+    const SharedOut<T> out(a, a.gc, a.gc_row, a.partc, a.chunks, at);
     for (int n = 0; n < at.nblk; ++n) {
         const int base = at.t0 + Q * n;
-        rbt.put(sb, tid);
-        rct.put(sc, tid);
-#pragma unroll
-        for (int k = 0; k < MINE; ++k)
-            if (w + NW * k < at.nh)
-                make_steps<Q, false>(ss[w + NW * k], dt_next[k], a.dt_bias ? a.dt_bias[at.h0 + w + NW * k] : 0.0f, a.rate[at.h0 + w + NW * k], true, lane);
-        fetch_dt(n + 1);
+        rbt.put(sb, pl, tid);
+        rct.put(sc, pl, tid);
         Op<RAW> v[QS];
         f4 O[IT], D[OWN];
 #pragma unroll
@@ -143,27 +187,24 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, 2
 #pragma unroll
         for (int k = 0; k < HB; ++k) {
             if (k >= at.nh) break;
-            rx.put(sx, tid);
-            ry.put(sy, tid);
+            rx.put(sx, pl, tid);
+            ry.put(sy, pl, tid);
             lds_barrier();
+            // the next head's rows, or the next block's
             {
-                // the next head's rows, or the next block's
                 const bool last = k + 1 >= at.nh;
-                const int next = last ? base + Q : base;
-                rx.base = x0 + (at.h0 + (last ? 0 : k + 1)) * a.P;
-                ry.base = y0 + (at.h0 + (last ? 0 : k + 1)) * a.P;
-                if (!last || n + 1 < at.nblk) {
-                    rx.fetch(next, at.L);
-                    ry.fetch(next, at.L);
-                    if (last) {
-                        rbt.fetch(next, at.L);
-                        rct.fetch(next, at.L);
-                    }
+                if (last) src.move(Q);
+                const int left = last ? at.L - base - Q : at.L - base, col = last ? 0 : (k + 1) * a.P * E;
+                rx.fetch(rows_at(src.x, left, Q, src.x_bytes), col);
+                ry.fetch(rows_at(src.y, left, Q, src.y_bytes), col);
+                if (last) {
+                    rbt.fetch(rows_at(src.b, left, Q, src.b_bytes), 0);
+                    rct.fetch(rows_at(src.c, left, Q, src.c_bytes), 0);
                 }
             }
             if (k == 0) {
 #pragma unroll
-                for (int ks = 0; ks < QS; ++ks) v[ks] = TL::by_col(sb, 32 * ks, 16 * w, lane);
+                for (int ks = 0; ks < QS; ++ks) v[ks] = TL::own_col(sb, ln, ks);
                 int own = 0;
 #pragma unroll
                 for (int m = 0; m < SC::TILES; ++m) {
@@ -171,14 +212,14 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, 2
                     f4 d = (f4)0.0f;
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks)
-                        d = mma(d, TL::by_row(sb, 16 * SC::keys(m) + i16, 32 * ks, g), TL::by_row(sc, 16 * SC::query(m) + i16, 32 * ks, g));
+                        d = mma(d, TL::by_row(sb, ln, SC::keys(m), ks), TL::by_row(sc, ln, SC::query(m), ks));
 #pragma unroll
                     for (int o = 0; o < OWN; ++o)
                         if (o == own) D[o] = d;
                     ++own;
                 }
             }
-            const Steps<Q> &s = ss[k];
+            const Steps<Q> &s = ss[n & 1][k];
             int own = 0;
 #pragma unroll
             for (int m = 0; m < SC::TILES; ++m) {
@@ -187,7 +228,7 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, 2
                 f4 p = (f4)0.0f, d = D[0];
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks)
-                    p = mma(p, TL::by_row(sx, 16 * jt + i16, 32 * ks, g), TL::by_row(sy, 16 * it + i16, 32 * ks, g));
+                    p = mma(p, TL::by_row(sx, ln, jt, ks), TL::by_row(sy, ln, it, ks));
                 p *= weights(s, it, jt, i16, g);
                 SC::put(sm, it, jt, p, lane);
 #pragma unroll
@@ -216,6 +257,8 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, 2
                     }
                 }
             }
+            if (w == NW - 1) make_steps<Q, false>(ss[(n + 1) & 1][k], dt[k].value(), bias[k], rate[k], true, lane);
+            fetch_dt(n + 2, k);
             // what the state at the block's start gives
             f4 F[IT];
 #pragma unroll
@@ -224,12 +267,12 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, 2
             for (int ks = 0; ks < KS; ++ks) {
                 const Op<HELD> st = split<HELD>(__builtin_shufflevector(S[k][2 * ks], S[k][2 * ks + 1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-                for (int it = 0; it < IT; ++it) F[it] = mma(F[it], st, TL::by_row(sy, 16 * it + i16, 32 * ks, g));
+                for (int it = 0; it < IT; ++it) F[it] = mma(F[it], st, TL::by_row(sy, ln, it, ks));
             }
 #pragma unroll
             for (int it = 0; it < IT; ++it) {
                 F[it] *= s.out[16 * it + i16];
-                const f4 e = F[it] * TL::four(sc, 16 * it + i16, 16 * w + 4 * g);
+                const f4 e = F[it] * TL::four(sc, ln, it);
                 const float sum = sum_rows(e[0] + e[1] + e[2] + e[3]);
                 if (g == 0) rp[w][16 * it + i16] = sum;
                 O[it] += F[it];
@@ -244,7 +287,7 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, 2
                     const f4 lo = *(const f4 *)(s.in + 32 * ks + 4 * g), hi = *(const f4 *)(s.in + 32 * ks + 16 + 4 * g);
                     const Op<HELD> u = split<HELD>(values(v[ks]) * __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-                    for (int kt = 0; kt < KT; ++kt) S[k][kt] = mma(S[k][kt], TL::by_col(sx, 32 * ks, 16 * kt, lane), u);
+                    for (int kt = 0; kt < KT; ++kt) S[k][kt] = mma(S[k][kt], TL::by_col(sx, ln, ks, kt), u);
                 }
             }
             lds_barrier();
@@ -252,125 +295,142 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, 2
             for (int it = 0; it < IT; ++it)
 #pragma unroll
                 for (int ks = 0; ks <= it / 2; ++ks) O[it] = mma(O[it], v[ks], SC::get(sm, SC::op(it, ks), lane));
-            if (w == k % NW) {
-                // lane = position; its sixteen is tile K
-                const int r = lane % Q, K = r >> 4, t = base + r;
-                float ri = 0.0f, before = 0.0f, after = 0.0f, own_t = 0.0f;
-                for (int x = 0; x < NW; ++x) ri += rp[x][r];
-                float span = 0.0f;
+            // sums over waves and tiles: each wave those of its sixteens, lane = position
+            const size_t line = (size_t)(at.b * a.H + at.h0 + k) * a.T;
 #pragma unroll
-                for (int m = 0; m < SC::TILES; ++m) {
-                    const int it = SC::query(m), jt = SC::keys(m);
-                    if (it == jt) {
-                        if (K == it) own_t = ends[m][i16];
-                    } else {
-                        const float e = ends[m][i16], b = starts[m][i16];
-                        if (K == it) after += e;
-                        if (K == jt) before += b;
-                        if (it - jt > 1) {
-                            const float whole = sum16(e);
-                            if (jt < K && K < it) span += whole;
+            for (int turn = 0; turn < TURNS; ++turn) {
+                const int K = w + NW * turn, at16 = 16 * K + i16;
+                float ri = 0.0f, dl = 0.0f;
+                if (K < IT) {
+                    float before = 0.0f, after = 0.0f;
+                    for (int x = 0; x < NW; ++x) ri += rp[x][at16];
+#pragma unroll
+                    for (int m = 0; m < SC::TILES; ++m) {
+                        const int it = SC::query(m), jt = SC::keys(m);
+                        if (it == jt) {
+                            if (K == it) dl += ends[m][i16];
+                        } else {
+                            if (K == it) after += ends[m][i16];
+                            if (K == jt) before += starts[m][i16];
+                            if (jt < K && K < it) dl += sum16(ends[m][i16]);
                         }
                     }
+                    dl += suffix16(after) + moved<0x111>(prefix16(before));
                 }
-                const float tail = suffix16(after), head = moved<0x111>(prefix16(before));
-                const size_t to = (size_t)(at.b * a.H + at.h0 + k) * a.T + t;
-                if (lane < Q && t < at.t1) {
-                    a.rint[to] = ri;
-                    a.dlin[to] = own_t + tail + head + span;
-                }
+                put_line<Q>(a.rint + line, base, at.t1, K < IT && g == 0 ? at16 : -1, ri);
+                put_line<Q>(a.dlin + line, base, at.t1, K < IT && g == 0 ? at16 : -1, dl);
             }
         }
 #pragma unroll
-        for (int it = 0; it < IT; ++it) store_shared<T>(a, a.gc, a.gc_row, a.partc, at, a.c_chunks, base + 16 * it + i16, 16 * w + 4 * g, O[it]);
-        // the first head's rows of the next block go where this block's last were read transposed by every wave: all have passed
-        // the barrier behind that
+        for (int it = 0; it < IT; ++it) out.template put<Q>(base, i16, 16 * it, 16 * w + 4 * g, a.N, at.t1, O[it]);
     }
-    if (a.c_chunks == 1)
+    if (a.chunks == 1)
         clear_rows<T>((T *)a.gc + at.rb * a.gc_row + at.grp * a.N, a.gc_row, at.t0 + at.nblk * Q, at.t1, a.N, tid, NT);
 }
 
 // ---- gradients of x and B -----------------------------------------------------------------------------------------
 //   du_j = sum_{i>=j} e^{c_i-c_j} (B_j . C_i) dy_i     queries B, keys C, values dy; state G [N x P]     dx = delta du + skip dy
 //   dB_j = sum_h delta_j sum_{i>=j} e^{c_i-c_j} (x_j . dy_i) C_i     queries x, keys dy, values C; state G^T [P x N]
-// Rows run backwards in time.  G is held both ways round, sixteen columns of each to a wave: twice the products for its
-// updates, and nothing to exchange.
-template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, 2) void k_ssm_grad_xb(SsmArgs a)
+// Rows run backwards in time.  A wave holds sixteen columns p of G; its parts, which the product with B needs anyway, go through
+// LDS, from where they are read transposed for the product with x.  Only float32 at a width of 128 has no room for that (98 KB):
+// there a wave holds sixteen columns n of the transpose as well, at twice the products for the updates.
+template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, waves_for(Parts<T>::raw, Q, DM)) void k_ssm_grad_xb(SsmArgs a)
 {
     constexpr int NT = DM * 4, NW = DM / 16, KT = DM / 16, KS = DM / 32, IT = Q / 16, QS = Q / 32;
-    constexpr int RAW = Parts<T>::raw, MADE = Parts<T>::made, HELD = 3;
+    constexpr int RAW = Parts<T>::raw, MADE = Parts<T>::made, HELD = 3, E = (int)sizeof(T);
     typedef Tile<T, Q, DM, NT, true> TL;
     typedef Scores<Q, MADE> SC;
-    constexpr int OWN = (SC::TILES + NW - 1) / NW;
-    __shared__ __attribute__((aligned(16))) __bf16 sx[TL::ELEMS];
-    __shared__ __attribute__((aligned(16))) __bf16 sy[TL::ELEMS];
-    __shared__ __attribute__((aligned(16))) __bf16 sb[TL::ELEMS];
-    __shared__ __attribute__((aligned(16))) __bf16 sc[TL::ELEMS];
-    __shared__ __attribute__((aligned(16))) __bf16 sm[2 * SC::ELEMS];
-    __shared__ __attribute__((aligned(16))) Steps<Q> ss[HB];
-    __shared__ float qp[NW][Q], xp[NW][Q];
+    constexpr int OWN = (SC::TILES + NW - 1) / NW, TURNS = (IT + NW - 1) / NW;
+    constexpr bool TWICE = RAW == 3 && DM == 128;
+    // one array, so that operands' places differ by constants
+    __shared__ __attribute__((aligned(16))) __bf16 pool[4 * TL::ELEMS + 2 * SC::ELEMS + (TWICE ? 0 : MADE * DM * DM)];
+    __bf16 *const sx = pool, *const sy = sx + TL::ELEMS, *const sb = sy + TL::ELEMS, *const sc = sb + TL::ELEMS, *const sm = sc + TL::ELEMS,
+        *const sg = sm + 2 * SC::ELEMS;  // G [p][n]
+    __shared__ __attribute__((aligned(16))) Steps<Q> ss[2][HB];
+    __shared__ float qp[2][NW][Q], xp[2][NW][Q];  // by wave: its columns' part of qint and x . du; of this head and the one before
 
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, i16 = lane & 15;
-    const Place<T> at(a, HB, Q, a.b_chunks);
+    const Place<T> at(a, HB, Q, a.chunks);
     if (!at.any) return;
     const size_t cells = (size_t)a.P * a.N;
-    const int c0 = 16 * w + i16;  // this lane's column: of P in G, of N in its transpose
-    const bool has_p = 16 * w < a.P, has_n = 16 * w < a.N;
+    const int c0 = 16 * w + i16;  // this lane's column
 
+    auto base_of = [&](int n) { return at.t0 + Q * (at.nblk - 1 - n); };
+    Sources<T> src(a, at, at.nblk ? base_of(0) : at.t0);
     TL rx, ry, rbt, rct;
-    rbt.init((const T *)a.b + at.rb * a.b_row + at.grp * a.N, a.b_row, a.N, tid);
-    rct.init((const T *)a.c + at.rb * a.c_row + at.grp * a.N, a.c_row, a.N, tid);
-    const T *x0 = (const T *)a.x + at.rb * a.x_row, *y0 = (const T *)a.gy + at.rb * a.gy_row;
-    rx.init(x0 + at.h0 * a.P, a.x_row, a.P, tid);
-    ry.init(y0 + at.h0 * a.P, a.gy_row, a.P, tid);
+    const typename TL::Lane ln(lane, w);
+    const typename TL::Place pl(tid);
+    rx.init(src.x_bytes, a.P, tid);
+    ry.init(src.y_bytes, a.P, tid);
+    rbt.init(src.b_bytes, a.N, tid);
+    rct.init(src.c_bytes, a.N, tid);
 
-    f4 S[HB][KT], R[HB][KT];  // G [n][p], and [p][n]
+    f4 S[HB][KT];                // G: rows n, this lane's column p
+    f4 R[TWICE ? HB : 1][TWICE ? KT : 1];  // its transpose: rows p, this lane's column n
+    float rate[HB], bias[HB], skip[HB], skip_sum[HB];
 #pragma unroll
     for (int k = 0; k < HB; ++k) {
-        const float *from = a.gs + ((size_t)(at.b * a.H + at.h0 + k) * (a.nseg + 1) + at.seg + 1) * cells;
-        const bool live = k < at.nh && at.nblk;
+        const int head = k < at.nh ? at.h0 + k : at.h0;
+        rate[k] = a.rate[head];
+        bias[k] = a.dt_bias ? a.dt_bias[head] : 0.0f;
+        skip[k] = a.skip ? a.skip[head] : 0.0f;
+        skip_sum[k] = 0.0f;
+        const float *from = a.gs + ((size_t)(at.b * a.H + head) * (a.nseg + 1) + at.seg + 1) * cells;
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
             const int row = 16 * kt + 4 * g;
-            S[k][kt] = live && row < a.N && c0 < a.P ? *(const f4 *)(from + (size_t)c0 * a.N + row) : (f4)0.0f;
-            R[k][kt] = (f4)0.0f;
+            S[k][kt] = at.nblk && row < a.N && c0 < a.P ? *(const f4 *)(from + (size_t)c0 * a.N + row) : (f4)0.0f;
+            if constexpr (TWICE) {
+                R[k][kt] = (f4)0.0f;
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (live && row + r < a.P && c0 < a.N) R[k][kt][r] = from[(size_t)(row + r) * a.N + c0];
+                for (int r = 0; r < 4; ++r)
+                    if (at.nblk && row + r < a.P && c0 < a.N) R[k][kt][r] = from[(size_t)(row + r) * a.N + c0];
+            }
         }
     }
-    constexpr int MINE = (HB + NW - 1) / NW;
-    float dt_next[MINE];
-    auto base_of = [&](int n) { return at.t0 + Q * (at.nblk - 1 - n); };
-    auto fetch_dt = [&](int n) {
-#pragma unroll
-        for (int k = 0; k < MINE; ++k) {
-            const int head = w + NW * k, t = base_of(n) + Q - 1 - lane % Q;
-            dt_next[k] = head < at.nh && n < at.nblk && t < at.L ? (float)((const T *)a.dt)[(at.rb + t) * a.dt_row + at.h0 + head] : -INFINITY;
-        }
+    Dt<T> dt[HB];
+    auto fetch_dt = [&](int n, int k) {
+        dt[k].fetch(src.dt + (k < at.nh ? k * E : 0) - (int64_t)Q * n * src.dt_bytes, src.dt_bytes, Q - 1 - lane % Q,
+                    n < at.nblk ? at.L - base_of(n) : 0);
     };
-    fetch_dt(0);
     if (at.nblk) {
-        const int base = base_of(0);
-        rbt.fetch(base, at.L);
-        rct.fetch(base, at.L);
-        rx.fetch(base, at.L);
-        ry.fetch(base, at.L);
+        const int left = at.L - base_of(0);
+        rbt.fetch(rows_at(src.b, left, Q, src.b_bytes), 0);
+        rct.fetch(rows_at(src.c, left, Q, src.c_bytes), 0);
+        rx.fetch(rows_at(src.x, left, Q, src.x_bytes), 0);
+        ry.fetch(rows_at(src.y, left, Q, src.y_bytes), 0);
         SC::clear(sm, tid, NT);
         SC::clear(sm + SC::ELEMS, tid, NT);
-    }
-    float skip_sum[HB];
 #pragma unroll
-    for (int k = 0; k < HB; ++k) skip_sum[k] = 0.0f;
+        for (int k = 0; k < HB; ++k) {
+            fetch_dt(0, k);
+            if (w == k % NW) make_steps<Q, true>(ss[0][k], dt[k].value(), bias[k], rate[k], false, lane);
+            fetch_dt(1, k);
+        }
+    }
+    const SharedOut<T> out(a, a.gb, a.gb_row, a.partb, a.chunks, at);
+    const int gx_bytes = (int)a.gx_row * E;
+    char *gxs = (char *)a.gx + (at.rb + (at.nblk ? base_of(0) : at.t0)) * gx_bytes + at.h0 * a.P * E;
+    const uint32_t gx_off = 16 * w + 4 * g < a.P ? (uint32_t)((15 - i16) * gx_bytes + (16 * w + 4 * g) * E) : OUTSIDE;
+    // The sums of a head over the waves are made while the next one is worked on: `turn` counts heads.
+    int turn = 0;
+    auto join = [&](int n, int k, bool any) {
+        const size_t line = (size_t)(at.b * a.H + at.h0 + k) * a.T;
+        const int p = (turn & 1) ^ 1, base = base_of(n);
+#pragma unroll
+        for (int x = 0; x < TURNS; ++x) {
+            const int K = w + NW * x, at16 = 16 * K + i16;
+            float q = 0.0f, s = 0.0f;
+            if (K < IT)
+                for (int y = 0; y < NW; ++y) q += qp[p][y][at16], s += xp[p][y][at16];
+            put_line<Q>(a.qint + line, base, at.t1, any && K < IT && g == 0 ? Q - 1 - at16 : -1, q);
+            put_line<Q>(a.xdu + line, base, at.t1, any && K < IT && g == 0 ? Q - 1 - at16 : -1, s);
+        }
+    };
     for (int n = 0; n < at.nblk; ++n) {
         const int base = base_of(n);
-        rbt.put(sb, tid);
-        rct.put(sc, tid);
-#pragma unroll
-        for (int k = 0; k < MINE; ++k)
-            if (w + NW * k < at.nh)
-                make_steps<Q, true>(ss[w + NW * k], dt_next[k], a.dt_bias ? a.dt_bias[at.h0 + w + NW * k] : 0.0f, a.rate[at.h0 + w + NW * k], false, lane);
-        fetch_dt(n + 1);
+        rbt.put(sb, pl, tid);
+        rct.put(sc, pl, tid);
         Op<RAW> vc[QS];
         f4 O[IT], D[OWN];
 #pragma unroll
@@ -378,26 +438,41 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, 2
 #pragma unroll
         for (int k = 0; k < HB; ++k) {
             if (k >= at.nh) break;
-            rx.put(sx, tid);
-            ry.put(sy, tid);
-            lds_barrier();
+            rx.put(sx, pl, tid);
+            ry.put(sy, pl, tid);
+            Op<HELD> st[KS];
             {
-                const bool last = k + 1 >= at.nh;
-                const int next = last ? base - Q : base;
-                rx.base = x0 + (at.h0 + (last ? 0 : k + 1)) * a.P;
-                ry.base = y0 + (at.h0 + (last ? 0 : k + 1)) * a.P;
-                if (!last || n + 1 < at.nblk) {
-                    rx.fetch(next, at.L);
-                    ry.fetch(next, at.L);
-                    if (last) {
-                        rbt.fetch(next, at.L);
-                        rct.fetch(next, at.L);
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    st[ks] = split<HELD>(__builtin_shufflevector(S[k][2 * ks], S[k][2 * ks + 1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                    for (int part = 0; part < (TWICE ? 0 : MADE); ++part) {
+                        const u4 v = __builtin_bit_cast(u4, st[ks].p[part]);
+                        __bf16 *to = sg + part * DM * DM + 16 * w * DM + ks / 2 * 64;
+                        *(u2 *)(to + ln.row[DM >= 64 ? ks % 2 * 2 : 0]) = (u2){v[0], v[1]};
+                        *(u2 *)(to + ln.row[DM >= 64 ? ks % 2 * 2 + 1 : 1]) = (u2){v[2], v[3]};
                     }
                 }
             }
+            lds_barrier();
+            {
+                const bool last = k + 1 >= at.nh;
+                if (last) src.move(-Q);
+                const int left = last ? Q : at.L - base, col = last ? 0 : (k + 1) * a.P * E;
+                if (!last || n + 1 < at.nblk) {
+                    rx.fetch(rows_at(src.x, left, Q, src.x_bytes), col);
+                    ry.fetch(rows_at(src.y, left, Q, src.y_bytes), col);
+                    if (last) {
+                        rbt.fetch(rows_at(src.b, left, Q, src.b_bytes), 0);
+                        rct.fetch(rows_at(src.c, left, Q, src.c_bytes), 0);
+                    }
+                }
+            }
+            if (k == 0) join(n > 0 ? n - 1 : 0, at.nh - 1, n > 0);
+            else join(n, k - 1, true);
             if (k == 0) {
 #pragma unroll
-                for (int ks = 0; ks < QS; ++ks) vc[ks] = TL::by_col(sc, 32 * ks, 16 * w, lane);
+                for (int ks = 0; ks < QS; ++ks) vc[ks] = TL::own_col(sc, ln, ks);
                 int own = 0;
 #pragma unroll
                 for (int m = 0; m < SC::TILES; ++m) {
@@ -405,14 +480,23 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, 2
                     f4 d = (f4)0.0f;
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks)
-                        d = mma(d, TL::by_row(sc, 16 * SC::keys(m) + i16, 32 * ks, g), TL::by_row(sb, 16 * SC::query(m) + i16, 32 * ks, g));
+                        d = mma(d, TL::by_row(sc, ln, SC::keys(m), ks), TL::by_row(sb, ln, SC::query(m), ks));
 #pragma unroll
                     for (int o = 0; o < OWN; ++o)
                         if (o == own) D[o] = d;
                     ++own;
                 }
             }
-            const Steps<Q> &s = ss[k];
+            const Steps<Q> &s = ss[n & 1][k];
+            f4 U[IT];
+            {
+#pragma unroll
+                for (int it = 0; it < IT; ++it) U[it] = (f4)0.0f;
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                    for (int it = 0; it < IT; ++it) U[it] = mma(U[it], st[ks], TL::by_row(sb, ln, it, ks));
+            }
             int own = 0;
 #pragma unroll
             for (int m = 0; m < SC::TILES; ++m) {
@@ -421,7 +505,7 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, 2
                 f4 p = (f4)0.0f, d = D[0];
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks)
-                    p = mma(p, TL::by_row(sy, 16 * jt + i16, 32 * ks, g), TL::by_row(sx, 16 * it + i16, 32 * ks, g));
+                    p = mma(p, TL::by_row(sy, ln, jt, ks), TL::by_row(sx, ln, it, ks));
                 if (it == jt) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) skip_sum[k] += 4 * g + r == i16 ? p[r] : 0.0f;
@@ -434,142 +518,122 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, 2
                 SC::put(sm, it, jt, d * f, lane);
                 SC::put(sm + SC::ELEMS, it, jt, p * (f * s.delta[16 * it + i16]), lane);
             }
+            if (w == NW - 1) make_steps<Q, true>(ss[(n + 1) & 1][k], dt[k].value(), bias[k], rate[k], false, lane);
+            fetch_dt(n + 2, k);
             // what the state behind the block gives to the gradient of B ..
-            if (has_n) {
+            {
                 f4 F[IT];
 #pragma unroll
                 for (int it = 0; it < IT; ++it) F[it] = (f4)0.0f;
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
-                    const Op<MADE> st = split<MADE>(__builtin_shufflevector(R[k][2 * ks], R[k][2 * ks + 1], 0, 1, 2, 3, 4, 5, 6, 7));
+                    Op<MADE> gt;
+                    if constexpr (TWICE) gt = split<MADE>(__builtin_shufflevector(R[k][2 * ks], R[k][2 * ks + 1], 0, 1, 2, 3, 4, 5, 6, 7));
+                    else gt = TL::template transposed<MADE>(sg, ln.own, 32 * ks * DM, DM * DM);
 #pragma unroll
-                    for (int it = 0; it < IT; ++it) F[it] = mma(F[it], st, TL::by_row(sx, 16 * it + i16, 32 * ks, g));
+                    for (int it = 0; it < IT; ++it) F[it] = mma(F[it], gt, TL::by_row(sx, ln, it, ks));
                 }
 #pragma unroll
                 for (int it = 0; it < IT; ++it) O[it] += F[it] * (s.out[16 * it + i16] * s.delta[16 * it + i16]);
             }
             // .. and to that of u
-            f4 U[IT];
+            f4 xv[IT], yv[IT];
             Op<RAW> vy[QS];
-            if (has_p) {
+            {
 #pragma unroll
-                for (int it = 0; it < IT; ++it) U[it] = (f4)0.0f;
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    const Op<HELD> st = split<HELD>(__builtin_shufflevector(S[k][2 * ks], S[k][2 * ks + 1], 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-                    for (int it = 0; it < IT; ++it) U[it] = mma(U[it], st, TL::by_row(sb, 16 * it + i16, 32 * ks, g));
-                }
-#pragma unroll
-                for (int ks = 0; ks < QS; ++ks) vy[ks] = TL::by_col(sy, 32 * ks, 16 * w, lane);
+                for (int ks = 0; ks < QS; ++ks) vy[ks] = TL::own_col(sy, ln, ks);
             }
 #pragma unroll
             for (int it = 0; it < IT; ++it) {
                 float sum = 0.0f;
-                if (has_p) {
+                {
                     U[it] *= s.out[16 * it + i16];
-                    const f4 e = U[it] * TL::four(sx, 16 * it + i16, 16 * w + 4 * g);
+                    xv[it] = TL::four(sx, ln, it);
+                    yv[it] = TL::four(sy, ln, it);
+                    const f4 e = U[it] * xv[it];
                     sum = sum_rows(e[0] + e[1] + e[2] + e[3]);
                 }
-                if (g == 0) qp[w][16 * it + i16] = sum * s.delta[16 * it + i16];
+                if (g == 0) qp[turn & 1][w][16 * it + i16] = sum * s.delta[16 * it + i16];
             }
-            // the state before the block, both ways round
+            // the state before the block
             {
                 const float keep = pow2(s.total);
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) S[k][kt] *= keep;
 #pragma unroll
                 for (int ks = 0; ks < QS; ++ks) {
                     const f4 lo = *(const f4 *)(s.in + 32 * ks + 4 * g), hi = *(const f4 *)(s.in + 32 * ks + 16 + 4 * g);
                     const f8 in = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                    if (has_p) {
-                        const Op<HELD> u = split<HELD>(values(vy[ks]) * in);
+                    const Op<HELD> u = split<HELD>(values(vy[ks]) * in);
 #pragma unroll
-                        for (int kt = 0; kt < KT; ++kt) {
-                            if (ks == 0) S[k][kt] *= keep;
-                            S[k][kt] = mma(S[k][kt], TL::by_col(sc, 32 * ks, 16 * kt, lane), u);
-                        }
-                    }
-                    if (has_n) {
-                        const Op<MADE> u = split<MADE>(values(vc[ks]) * in);
+                    for (int kt = 0; kt < KT; ++kt) S[k][kt] = mma(S[k][kt], TL::by_col(sc, ln, ks, kt), u);
+                    if constexpr (TWICE) {
+                        const Op<MADE> v = split<MADE>(values(vc[ks]) * in);
 #pragma unroll
-                        for (int kt = 0; kt < KT; ++kt) {
-                            if (ks == 0) R[k][kt] *= keep;
-                            R[k][kt] = mma(R[k][kt], TL::by_col(sy, 32 * ks, 16 * kt, lane), u);
-                        }
+                        for (int kt = 0; kt < KT; ++kt) R[k][kt] = mma(ks ? R[k][kt] : R[k][kt] * keep, TL::by_col(sy, ln, ks, kt), v);
                     }
                 }
             }
-            const float skip = a.skip ? a.skip[at.h0 + k] : 0.0f;
             lds_barrier();
-            if (has_n) {
+            {
 #pragma unroll
                 for (int it = 0; it < IT; ++it)
 #pragma unroll
                     for (int ks = 0; ks <= it / 2; ++ks) O[it] = mma(O[it], vc[ks], SC::get(sm + SC::ELEMS, SC::op(it, ks), lane));
             }
-            if (has_p) {
-                const int col = 16 * w + 4 * g;
 #pragma unroll
-                for (int it = 0; it < IT; ++it) {
+            for (int it = 0; it < IT; ++it) {
+                const int r = 16 * it + i16;
+                float sum = 0.0f;
+                f4 o = (f4)0.0f;
+                {
 #pragma unroll
                     for (int ks = 0; ks <= it / 2; ++ks) U[it] = mma(U[it], vy[ks], SC::get(sm, SC::op(it, ks), lane));
-                    const int r = 16 * it + i16, t = base + Q - 1 - r;
-                    const f4 e = U[it] * TL::four(sx, r, 16 * w + 4 * g), o = U[it] * s.delta[r] + TL::four(sy, r, 16 * w + 4 * g) * skip;
-                    const float sum = sum_rows(e[0] + e[1] + e[2] + e[3]);
-                    if (g == 0) xp[w][r] = sum;
-                    const float out[4] = {o[0], o[1], o[2], o[3]};
-                    if (t < at.t1 && col < a.P) store_n<T, 4>((T *)a.gx + (at.rb + t) * a.gx_row + (at.h0 + k) * a.P + col, out);
+                    const f4 e = U[it] * xv[it];
+                    o = U[it] * s.delta[r] + yv[it] * skip[k];
+                    sum = sum_rows(e[0] + e[1] + e[2] + e[3]);
                 }
-            } else {
-#pragma unroll
-                for (int it = 0; it < IT; ++it)
-                    if (g == 0) xp[w][16 * it + i16] = 0.0f;
+                if (g == 0) xp[turn & 1][w][r] = sum;
+                store_four<T>(rows_at(gxs, at.t1 - base, Q, gx_bytes), gx_off, 16 * (IT - 1 - it) * gx_bytes + k * a.P * E, o);
             }
-            lds_barrier();
-            if (w == k % NW) {
-                const int r = lane % Q, t = base + Q - 1 - r;
-                float q = 0.0f, x = 0.0f;
-                for (int y = 0; y < NW; ++y) q += qp[y][r], x += xp[y][r];
-                const size_t to = (size_t)(at.b * a.H + at.h0 + k) * a.T + t;
-                if (lane < Q && t < at.t1) {
-                    a.qint[to] = q;
-                    a.xdu[to] = x;
-                }
-            }
+            ++turn;
         }
+        gxs -= (int64_t)Q * gx_bytes;
 #pragma unroll
-        for (int it = 0; it < IT; ++it) store_shared<T>(a, a.gb, a.gb_row, a.partb, at, a.b_chunks, base + Q - 1 - 16 * it - i16, 16 * w + 4 * g, O[it]);
+        for (int it = 0; it < IT; ++it) out.template put<Q>(base, 15 - i16, 16 * (IT - 1 - it), 16 * w + 4 * g, a.N, at.t1, O[it]);
     }
+    lds_barrier();
+    if (at.nblk) join(at.nblk - 1, at.nh - 1, true);
     // sums for the skip: by wave in LDS, then over the waves in order
     lds_barrier();
 #pragma unroll
     for (int k = 0; k < HB; ++k) {
         for (int d = 1; d < 64; d *= 2) skip_sum[k] += __shfl_xor(skip_sum[k], d);
-        if (lane == 0) qp[w][k] = skip_sum[k];
+        if (lane == 0) qp[0][w][k] = skip_sum[k];
     }
     lds_barrier();
     if (tid < at.nh) {
         float s = 0.0f;
-        for (int y = 0; y < NW; ++y) s += qp[y][tid];
+        for (int y = 0; y < NW; ++y) s += qp[0][y][tid];
         a.skipp[(size_t)(at.b * a.H + at.h0 + tid) * a.nseg + at.seg] = s;
     }
     clear_rows<T>((T *)a.gx + at.rb * a.gx_row + at.h0 * a.P, a.gx_row, at.t0 + at.nblk * Q, at.t1, at.nh * a.P, tid, NT);
-    if (a.b_chunks == 1)
+    if (a.chunks == 1)
         clear_rows<T>((T *)a.gb + at.rb * a.gb_row + at.grp * a.N, a.gb_row, at.t0 + at.nblk * Q, at.t1, a.N, tid, NT);
 }
 
 template <class T, int Q, int DM> int launch_grad(const SsmArgs &a, hipStream_t st)
 {
-    const long units = ((long)a.B * a.nseg + 7) / 8 * 8 * a.G;
-    if (units * a.b_chunks > 0x7fffffffL) return SEMICRF_EUNSUPPORTED;
-    const dim3 gc((unsigned)(units * a.c_chunks)), gx((unsigned)(units * a.b_chunks)), t(DM * 4);
-    if constexpr (DM <= 64) {
-        if (a.c_heads > 1) hipLaunchKernelGGL((k_ssm_grad_c<T, Q, DM, 4>), gc, t, 0, st, a);
-        else hipLaunchKernelGGL((k_ssm_grad_c<T, Q, DM, 1>), gc, t, 0, st, a);
-        if (a.b_heads > 1) hipLaunchKernelGGL((k_ssm_grad_xb<T, Q, DM, 2>), gx, t, 0, st, a);
-        else hipLaunchKernelGGL((k_ssm_grad_xb<T, Q, DM, 1>), gx, t, 0, st, a);
+    const long grid = ((long)a.B * a.nseg + 7) / 8 * 8 * a.G * a.chunks;
+    if (grid > 0x7fffffffL) return SEMICRF_EUNSUPPORTED;
+    const dim3 g((unsigned)grid), t(DM * 4);
+    constexpr int HB = DM <= 64 ? GRAD_HEADS : 1;
+    if (a.heads > 1) {
+        hipLaunchKernelGGL((k_ssm_grad_c<T, Q, DM, HB>), g, t, 0, st, a);
+        hipLaunchKernelGGL((k_ssm_grad_xb<T, Q, DM, HB>), g, t, 0, st, a);
     } else {
-        hipLaunchKernelGGL((k_ssm_grad_c<T, Q, DM, 1>), gc, t, 0, st, a);
-        hipLaunchKernelGGL((k_ssm_grad_xb<T, Q, DM, 1>), gx, t, 0, st, a);
+        hipLaunchKernelGGL((k_ssm_grad_c<T, Q, DM, 1>), g, t, 0, st, a);
+        hipLaunchKernelGGL((k_ssm_grad_xb<T, Q, DM, 1>), g, t, 0, st, a);
     }
     return launched();
 }

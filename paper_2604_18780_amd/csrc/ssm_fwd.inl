@@ -24,10 +24,9 @@ template <class T, int Q, int DK, int PV, bool OUT, bool REV> __global__ __launc
     typedef Tile<T, Q, DK, NT, REV> TK;
     typedef Tile<T, Q, PV, NT, REV> TV;
     typedef Scores<Q, MADE> SC;
-    __shared__ __attribute__((aligned(16))) __bf16 sq[OUT ? TK::ELEMS : 8];
-    __shared__ __attribute__((aligned(16))) __bf16 sk[TK::ELEMS];
-    __shared__ __attribute__((aligned(16))) __bf16 sv[TV::ELEMS];
-    __shared__ __attribute__((aligned(16))) __bf16 sm[OUT ? SC::ELEMS : 8];
+    // one array, so that operands' places differ by constants
+    __shared__ __attribute__((aligned(16))) __bf16 pool[(OUT ? 2 : 1) * TK::ELEMS + TV::ELEMS + (OUT ? SC::ELEMS : 0)];
+    __bf16 *const sk = pool, *const sv = sk + TK::ELEMS, *const sq = sv + TV::ELEMS, *const sm = sq + (OUT ? TK::ELEMS : 0);
     __shared__ __attribute__((aligned(16))) Steps<Q> ss[AHEAD];
 
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, i16 = lane & 15;
@@ -43,12 +42,25 @@ template <class T, int Q, int DK, int PV, bool OUT, bool REV> __global__ __launc
 
     TK rq, rk;
     TV rv;
-    const T *qb = (const T *)a.c + rb * a.c_row + grp * a.N, *kb = (const T *)a.b + rb * a.b_row + grp * a.N;
-    if constexpr (OUT) rq.init(qb, a.c_row, a.N, tid);
-    rk.init(REV ? qb : kb, REV ? a.c_row : a.b_row, a.N, tid);
-    rv.init((REV ? (const T *)a.gy + rb * a.gy_row : (const T *)a.x + rb * a.x_row) + h * a.P, REV ? a.gy_row : a.x_row, a.P, tid);
+    const typename TK::Lane lk(lane, 0);
+    const typename TV::Lane lv(lane, w);
+    const typename TK::Place pk(tid);
+    const typename TV::Place pv(tid);
+    // rows from the first block on; each block moves on (back) by Q of them
+    const int qk_bytes = (int)(a.c_row * (int64_t)sizeof(T)), b_bytes = (int)(a.b_row * (int64_t)sizeof(T));
+    const int v_bytes = (int)((REV ? a.gy_row : a.x_row) * (int64_t)sizeof(T)), dt_bytes = (int)(a.dt_row * (int64_t)sizeof(T));
+    const int y_bytes = (int)(a.y_row * (int64_t)sizeof(T)), k_bytes = REV ? qk_bytes : b_bytes;
+    const int64_t start = rb + t0 + (REV && nblk ? Q * (nblk - 1) : 0);
+    const char *cs = (const char *)a.c + start * qk_bytes + grp * a.N * (int)sizeof(T);
+    const char *kb = REV ? cs : (const char *)a.b + start * b_bytes + grp * a.N * (int)sizeof(T);
+    const char *vs = (const char *)(REV ? a.gy : a.x) + start * v_bytes + h * a.P * (int)sizeof(T);
+    const char *dts = (const char *)a.dt + (rb + t0) * dt_bytes + h * (int)sizeof(T);
+    char *ys = (char *)a.y + (rb + t0) * y_bytes + h * a.P * (int)sizeof(T);
+    constexpr int DIR = REV ? -Q : Q;
+    if constexpr (OUT) rq.init(qk_bytes, a.N, tid);
+    rk.init(k_bytes, a.N, tid);
+    rv.init(v_bytes, a.P, tid);
     const float rate = a.rate[h], bias = a.dt_bias ? a.dt_bias[h] : 0.0f, skip = OUT && a.skip ? a.skip[h] : 0.0f;
-    const T *dts = (const T *)a.dt + rb * a.dt_row + h;
 
     // state: rows n (16 kt + 4g + r), column p = 16 w + lane % 16; memory is [P][N]
     const int p = 16 * w + i16;
@@ -63,51 +75,55 @@ template <class T, int Q, int DK, int PV, bool OUT, bool REV> __global__ __launc
 
     double gone = 0.0;
     auto at = [&](int n) { return t0 + Q * (REV ? nblk - 1 - n : n); };
-    auto dt_of = [&](int n) {
-        const int r = lane % Q, t = at(n) + (REV ? Q - 1 - r : r);
-        return n < nblk && t < L ? (float)dts[t * a.dt_row] : -INFINITY;
+    Dt<T> dt_next;  // of the block this wave makes the steps of
+    auto fetch_dt = [&](int n) {
+        const int r = lane % Q, first = at(n) - t0;
+        dt_next.fetch(dts + (int64_t)first * dt_bytes, dt_bytes, REV ? Q - 1 - r : r, n < nblk ? L - at(n) : 0);
     };
-    const uint32_t y_off = 16 * w + 4 * g < a.P ? (uint32_t)(i16 * a.y_row + 16 * w + 4 * g) * (uint32_t)sizeof(T) : OUTSIDE;
+    auto fetch = [&](int n) {
+        const int left = L - at(n);
+        if constexpr (OUT) rq.fetch(rows_at(cs, left, Q, qk_bytes), 0);
+        rk.fetch(rows_at(kb, left, Q, k_bytes), 0);
+        rv.fetch(rows_at(vs, left, Q, v_bytes), 0);
+        cs += (int64_t)DIR * qk_bytes;
+        kb += (int64_t)DIR * k_bytes;
+        vs += (int64_t)DIR * v_bytes;
+    };
+    const uint32_t y_off = 16 * w + 4 * g < a.P ? (uint32_t)(i16 * y_bytes + (16 * w + 4 * g) * (int)sizeof(T)) : OUTSIDE;
     f4 skips;  // on the diagonal of the scores
 #pragma unroll
     for (int r = 0; r < 4; ++r) skips[r] = 4 * g + r == i16 ? skip : 0.0f;
-    float dt_next = dt_of(w);  // of the block this wave makes the steps of
+    fetch_dt(w);
     if (nblk) {
-        if constexpr (OUT) rq.fetch(at(0), L);
-        rk.fetch(at(0), L);
-        rv.fetch(at(0), L);
+        fetch(0);
         if constexpr (OUT) SC::clear(sm, tid, NT);
     }
     for (int n = 0; n < nblk; ++n) {
         const int base = at(n);
         const Steps<Q> &s = ss[n % AHEAD];
         if (n % AHEAD == 0 && w < AHEAD) {
-            make_steps<Q, REV>(ss[w], dt_next, bias, rate, !REV, lane);
-            dt_next = dt_of(n + AHEAD + w);
+            make_steps<Q, REV>(ss[w], dt_next.value(), bias, rate, !REV, lane);
+            fetch_dt(n + AHEAD + w);
         }
-        if constexpr (OUT) rq.put(sq, tid);
-        rk.put(sk, tid);
-        rv.put(sv, tid);
+        if constexpr (OUT) rq.put(sq, pk, tid);
+        rk.put(sk, pk, tid);
+        rv.put(sv, pv, tid);
         lds_barrier();
-        if (n + 1 < nblk) {
-            if constexpr (OUT) rq.fetch(at(n + 1), L);
-            rk.fetch(at(n + 1), L);
-            rv.fetch(at(n + 1), L);
-        }
+        if (n + 1 < nblk) fetch(n + 1);
         f4 O[IT];
         if constexpr (OUT) {
             Op<RAW> q[IT][KS];
 #pragma unroll
             for (int it = 0; it < IT; ++it)
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) q[it][ks] = TK::by_row(sq, 16 * it + i16, 32 * ks, g);
+                for (int ks = 0; ks < KS; ++ks) q[it][ks] = TK::by_row(sq, lk, it, ks);
 #pragma unroll
             for (int k = 0; k < SC::TILES; ++k) {
                 if (SC::wave(k, NW) != w) continue;
                 const int it = SC::query(k), jt = SC::keys(k);
                 f4 m = (f4)0.0f;
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) m = mma(m, TK::by_row(sk, 16 * jt + i16, 32 * ks, g), q[it][ks]);
+                for (int ks = 0; ks < KS; ++ks) m = mma(m, TK::by_row(sk, lk, jt, ks), q[it][ks]);
                 m *= weights(s, it, jt, i16, g);
                 if (it == jt) m += skips;
                 SC::put(sm, it, jt, m, lane);
@@ -126,7 +142,7 @@ template <class T, int Q, int DK, int PV, bool OUT, bool REV> __global__ __launc
         }
         Op<RAW> v[QS];
 #pragma unroll
-        for (int ks = 0; ks < QS; ++ks) v[ks] = TV::by_col(sv, 32 * ks, 16 * w, lane);
+        for (int ks = 0; ks < QS; ++ks) v[ks] = TV::own_col(sv, lv, ks);
         // the state at the block's end
         {
             const float keep = pow2(s.total);
@@ -137,7 +153,7 @@ template <class T, int Q, int DK, int PV, bool OUT, bool REV> __global__ __launc
                 const f4 lo = *(const f4 *)(s.in + 32 * ks + 4 * g), hi = *(const f4 *)(s.in + 32 * ks + 16 + 4 * g);
                 const Op<HELD> u = split<HELD>(values(v[ks]) * __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-                for (int kt = 0; kt < KT; ++kt) S[kt] = mma(S[kt], TK::by_col(sk, 32 * ks, 16 * kt, lane), u);
+                for (int kt = 0; kt < KT; ++kt) S[kt] = mma(S[kt], TK::by_col(sk, lk, ks, kt), u);
             }
             gone += s.total;
         }
@@ -148,15 +164,10 @@ template <class T, int Q, int DK, int PV, bool OUT, bool REV> __global__ __launc
 #pragma unroll
                 for (int ks = 0; ks <= it / 2; ++ks) O[it] = mma(O[it], v[ks], SC::get(sm, SC::op(it, ks), lane));
             // a lane holds channels 16 w + 4g .. +3 of positions i16, 16 + i16, ..
-            const __amdgpu_buffer_rsrc_t rows = rows_from((const T *)a.y + (rb + base) * a.y_row + h * a.P, (t1 - base) * a.y_row * (int64_t)sizeof(T));
+            const __amdgpu_buffer_rsrc_t rows = rows_at(ys, t1 - base, Q, y_bytes);
+            ys += (int64_t)Q * y_bytes;
 #pragma unroll
-            for (int it = 0; it < IT; ++it) {
-                typedef T T4 __attribute__((ext_vector_type(4)));
-                const T4 o = __builtin_convertvector(O[it], T4);
-                const int from_row = (int)(16 * it * a.y_row * (int64_t)sizeof(T));
-                if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, o), rows, (int)y_off, from_row, 0);
-                else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u2, o), rows, (int)y_off, from_row, 0);
-            }
+            for (int it = 0; it < IT; ++it) store_four<T>(rows, y_off, 16 * it * y_bytes, O[it]);
         }
     }
 
