@@ -56,14 +56,19 @@ __device__ __forceinline__ float exp_of(float v)
     return __builtin_fmaf(e, l * 0.693147181f, e);
 }
 
-// ln(1 + e^v) without overflow, and its derivative.
+// ln(1 + e^v) without overflow, and its derivative.  With e = e^-|v| and s = e / (2 + e) <= 1/3, ln(1 + e) = 2 artanh(s), of which
+// seven terms hold 2^-26; the hardware's logarithm loses digits where 1 + e is near 1.
 __device__ __forceinline__ float softplus(float v)
 {
-    const float e = exp_of(fmaxf(-fabsf(v), -100.0f)), u = 1.0f + e;
-    // for small e the series, to 2^-27 of its value; else the logarithm, with what 1 + e has lost put back
-    const float small = e * __builtin_fmaf(e, __builtin_fmaf(e, __builtin_fmaf(e, __builtin_fmaf(e, 0.2f, -0.25f), 0.333333333f), -0.5f), 1.0f);
-    const float large = __builtin_fmaf(e - (u - 1.0f), __builtin_amdgcn_rcpf(u), 0.693147181f * __builtin_amdgcn_logf(u));
-    return fmaxf(v, 0.0f) + (e < 0.03125f ? small : large);
+    const float e = exp_of(fmaxf(-fabsf(v), -100.0f)), d = 2.0f + e;
+    const float r = __builtin_amdgcn_rcpf(d), q = e * r, s = __builtin_fmaf(__builtin_fmaf(-q, d, e), r, q), z = s * s;
+    float p = __builtin_fmaf(z, 1.0f / 13.0f, 1.0f / 11.0f);
+    p = __builtin_fmaf(p, z, 1.0f / 9.0f);
+    p = __builtin_fmaf(p, z, 1.0f / 7.0f);
+    p = __builtin_fmaf(p, z, 0.2f);
+    p = __builtin_fmaf(p, z, 1.0f / 3.0f);
+    p = __builtin_fmaf(p * z, s, s);
+    return __builtin_fmaf(2.0f, p, fmaxf(v, 0.0f));
 }
 __device__ __forceinline__ float sigmoid(float v)
 {

@@ -41,6 +41,7 @@ struct SsmArgs {
     float *partc, *partb;     // [chunks][B*T][G][N] gradients of C and B by workgroup, where there are several
     float *rint, *dlin, *qint, *xdu;  // [B*H][T] see k_ssm_steps
     float *skipp;             // [B*H][nseg]
+    double *cross;            // [B*H][nseg+1] pairs that cross a segment's boundary
     double *headp;            // [B*H*nseg][2] sums for rate and bias
 };
 

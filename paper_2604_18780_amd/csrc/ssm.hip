@@ -41,64 +41,99 @@ template <bool REV> __global__ __launch_bounds__(256) void k_ssm_chain(SsmArgs a
     if (last) *(f4 *)(last + bh * cells + at) = h;
 }
 
+// Pairs of positions that cross a segment's boundary: <G, H> there, G the gradient of the state H.  One wave per boundary.
+__global__ __launch_bounds__(256) void k_ssm_cross(SsmArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const size_t at = (size_t)blockIdx.x * 4 + threadIdx.x / 64, cells = (size_t)a.P * a.N;
+    if (at >= (size_t)a.B * a.H * (a.nseg + 1)) return;
+    const f4 *hs = (const f4 *)(a.hs + at * cells), *gs = (const f4 *)(a.gs + at * cells);
+    double s = 0.0;
+    for (size_t k = lane; k < cells / 4; k += 64) {
+        const f4 p = hs[k], q = gs[k];
+        s += (double)p[0] * q[0] + (double)p[1] * q[1] + (double)p[2] * q[2] + (double)p[3] * q[3];
+    }
+    for (int d = 1; d < 64; d *= 2) s += __shfl_xor(s, d);
+    if (lane == 0) a.cross[at] = s;
+}
+
 // Gradients of the steps.  l_t multiplies everything that passes step t: pairs (i, j) with j < t <= i, of four kinds by block:
 //   dlin[t]  both ends in t's block,
 //   rint[i]  from before the block to i in it; those with i >= t count,
 //   qint[j]  from j in the block to behind it; those with j < t count,
 //   across   from before the block to behind it.
-// At a segment's end all pairs that cross it are <G, H>; from there backwards, taking off those that begin in a block leaves
-// its `across`, and adding those that end in it gives what crosses its start.  Where a block keeps less than 2^-30, nothing
-// is left of the difference but its rounding: `across` is 0.  One wave per (sequence, head, segment).
+// The pairs that cross a boundary are known at a segment's ends (k_ssm_cross).  From the later one backwards, taking off those that
+// begin in a block leaves its `across`, and adding those that end in it gives what crosses its start.  Rounding adds up along that
+// walk, and all positions of a block share it: what the walk is off by at the segment's start is taken back in equal parts.
+// Where a block keeps less than 2^-30, nothing is left of the difference but rounding: `across` is 0, and the walk begins
+// anew.  One wave per (sequence, head, segment).
+constexpr int MOST_BLOCKS = 16;  // of a segment of 512
+
 template <class T> __global__ __launch_bounds__(64) void k_ssm_steps(SsmArgs a)
 {
+    __shared__ double over[MOST_BLOCKS];
     const int lane = threadIdx.x, Q = a.block, r = lane & (Q - 1);
     const int seg = blockIdx.x % a.nseg, bh = blockIdx.x / a.nseg, h = bh % a.H, b = bh / a.H;
     const int L = length_of(a.lengths, b, a.T);
     const int t0 = seg * a.seg, t1 = t0 + a.seg < a.T ? t0 + a.seg : a.T;
     const int used = (t1 < L ? t1 : L) - t0, nblk = used > 0 ? (used + Q - 1) / Q : 0;
-    const size_t cells = (size_t)a.P * a.N;
     T *gdt = (T *)a.gdt + (int64_t)b * a.T * a.gdt_row + h;
     const T *dts = (const T *)a.dt + (int64_t)b * a.T * a.dt_row + h;
     const float rate = a.rate[h], bias = a.dt_bias ? a.dt_bias[h] : 0.0f;
-    double across = 0.0, grate = 0.0, gbias = 0.0;
-    if (nblk) {
-        const f4 *hs = (const f4 *)(a.hs + ((size_t)bh * (a.nseg + 1) + seg + 1) * cells);
-        const f4 *gs = (const f4 *)(a.gs + ((size_t)bh * (a.nseg + 1) + seg + 1) * cells);
-        for (size_t k = lane; k < cells / 4; k += 64) {
-            const f4 p = hs[k], q = gs[k];
-            across += (double)p[0] * q[0] + (double)p[1] * q[1] + (double)p[2] * q[2] + (double)p[3] * q[3];
+    const double *cross = a.cross + (size_t)bh * (a.nseg + 1) + seg;
+    {
+        double across = cross[1];
+        int first = nblk;  // the walk's blocks: up to here
+        for (int n = nblk - 1; n >= 0; --n) {
+            const int t = t0 + Q * n + lane;
+            const bool in = lane < Q && t < L && t < t1;
+            const size_t at = (size_t)bh * a.T + t;
+            float kept = in ? softplus((float)dts[t * a.dt_row] + bias) : 0.0f;
+            double ri = in ? (double)a.rint[at] : 0.0, qi = in ? (double)a.qint[at] : 0.0;
+            for (int d = 1; d < 64; d *= 2) kept += __shfl_xor(kept, d), ri += __shfl_xor(ri, d), qi += __shfl_xor(qi, d);
+            const bool gone = kept * rate * 1.44269504f < -30.0f;
+            const double off = gone ? across - qi : n == 0 ? across - qi + ri - cross[0] : 0.0;
+            across -= qi;
+            if (lane == 0) over[n] = across;
+            if (gone || n == 0) {
+                // spread over the blocks from `first` down to this one: the later, the less of it has come together
+                __syncthreads();
+                const int m = first - n;
+                if (lane < m) over[n + lane] -= off * (double)(m - lane) / m;
+                if (gone && lane == 0) over[n] = 0.0;
+                __syncthreads();
+                first = n;
+                across = 0.0;
+            }
+            across += ri;
         }
-        for (int d = 1; d < 64; d *= 2) across += __shfl_xor(across, d);
     }
-    for (int n = nblk - 1; n >= 0; --n) {
+    __syncthreads();
+    double grate = 0.0, gbias = 0.0;
+    for (int n = 0; n < nblk; ++n) {
         const int t = t0 + Q * n + r;
         const bool in = t < L && t < t1;
         const size_t at = (size_t)bh * a.T + t;
-        float ri = 0.0f, qi = 0.0f, own = 0.0f, dx = 0.0f, raw = 0.0f, delta = 0.0f;
+        float tail = 0.0f, qi = 0.0f, own = 0.0f, dx = 0.0f, raw = 0.0f;
         if (in) {
-            ri = a.rint[at], own = a.dlin[at], qi = a.qint[at], dx = a.xdu[at];
+            tail = a.rint[at], own = a.dlin[at], qi = a.qint[at], dx = a.xdu[at];
             raw = (float)dts[t * a.dt_row] + bias;
-            delta = softplus(raw);
         }
         // over the block's lanes (the other half of the wave repeats them where a block is 32)
-        float tail = ri, head = __shfl_up(qi, 1), kept = delta;
+        float head = __shfl_up(qi, 1);
         if (r == 0) head = 0.0f;
         for (int d = 1; d < Q; d *= 2) {
             const float o = __shfl_down(tail, d), p = __shfl_up(head, d);
             if (r + d < Q) tail += o;
             if (r >= d) head += p;
-            kept += __shfl_xor(kept, d);
         }
-        const float all_r = __shfl(tail, 0), all_q = __shfl(head + qi, Q - 1);
-        across = kept * rate * 1.44269504f < -30.0f ? 0.0 : across - all_q;
         if (in && lane < Q) {
-            const float dl = own + tail + head + (float)across, g = (dx + rate * dl) * sigmoid(raw);
+            const float dl = own + tail + head + (float)over[n], g = (dx + rate * dl) * sigmoid(raw);
             const float one[1] = {g};
             store_n<T, 1>(gdt + t * a.gdt_row, one);
-            grate += (double)dl * delta;
+            grate += (double)dl * softplus(raw);
             gbias += (double)g;
         }
-        across += all_r;
     }
     for (int t = (used > 0 ? t0 + used : t0) + lane; t < t1; t += 64) gdt[t * a.gdt_row] = (T)0.0f;
     for (int d = 1; d < 64; d *= 2) grate += __shfl_xor(grate, d), gbias += __shfl_xor(gbias, d);
@@ -245,7 +280,7 @@ template <class T> __global__ __launch_bounds__(256) void k_ssm_step(StepArgs a)
 
 struct SsmPlan {
     int seg, nseg, heads, chunks;
-    size_t hs, gs, kept, partc, partb, rint, dlin, qint, xdu, skipp, headp, total;
+    size_t hs, gs, kept, partc, partb, rint, dlin, qint, xdu, skipp, cross, headp, total;
 };
 
 // Positions of a segment of a forward call.
@@ -273,7 +308,7 @@ int make_ssm_plan(int B, int T, int H, int P, int G, int N, bool grad, SsmPlan *
         p->heads = room && groups * ((hpg + GRAD_HEADS - 1) / GRAD_HEADS) >= 512 ? GRAD_HEADS : 1;
         p->chunks = (hpg + p->heads - 1) / p->heads;
         p->seg = segment_length(B, T, G * p->chunks);
-        if (p->seg > 512) p->seg = 512;
+        if (p->seg > 32 * MOST_BLOCKS) p->seg = 32 * MOST_BLOCKS;
     }
     p->nseg = (T + p->seg - 1) / p->seg;
     size_t at = 0;
@@ -295,6 +330,7 @@ int make_ssm_plan(int B, int T, int H, int P, int G, int N, bool grad, SsmPlan *
         p->qint = take(rows * H * 4);
         p->xdu = take(rows * H * 4);
         p->skipp = take(bh * p->nseg * 4);
+        p->cross = take(bh * (p->nseg + 1) * 8);
         p->headp = take(bh * p->nseg * 16);
     }
     p->total = at;
@@ -410,6 +446,7 @@ int semicrf_ssm_bwd(const void *x, int64_t x_row, const void *b, int64_t b_row, 
     a.partc = (float *)(w + p.partc); a.partb = (float *)(w + p.partb);
     a.rint = (float *)(w + p.rint); a.dlin = (float *)(w + p.dlin); a.qint = (float *)(w + p.qint);
     a.xdu = (float *)(w + p.xdu); a.skipp = (float *)(w + p.skipp); a.headp = (double *)(w + p.headp);
+    a.cross = (double *)(w + p.cross);
     const hipStream_t st = (hipStream_t)stream;
     const int most = P > N ? P : N;
     a.heads = p.heads; a.chunks = p.chunks;
@@ -419,6 +456,7 @@ int semicrf_ssm_bwd(const void *x, int64_t x_row, const void *b, int64_t b_row, 
     if (int rc = chain(false, a, st)) return rc;
     if (int rc = chain(true, a, st)) return rc;
     if (int rc = grad(type, a, st)) return rc;
+    hipLaunchKernelGGL(k_ssm_cross, dim3((unsigned)(((int64_t)B * H * (p.nseg + 1) + 3) / 4)), dim3(256), 0, st, a);
     const dim3 steps(B * H * p.nseg), heads((unsigned)(((int64_t)B * T * G * (N / 4) + 255) / 256), 2);
     if (type == ACT_BF16) {
         hipLaunchKernelGGL((k_ssm_steps<__bf16>), steps, dim3(64), 0, st, a);

@@ -212,7 +212,7 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
                     f4 d = (f4)0.0f;
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks)
-                        d = mma(d, TL::by_row(sb, ln, SC::keys(m), ks), TL::by_row(sc, ln, SC::query(m), ks));
+                        d = mma_inputs(d, TL::by_row(sb, ln, SC::keys(m), ks), TL::by_row(sc, ln, SC::query(m), ks));
 #pragma unroll
                     for (int o = 0; o < OWN; ++o)
                         if (o == own) D[o] = d;
@@ -228,7 +228,7 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
                 f4 p = (f4)0.0f, d = D[0];
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks)
-                    p = mma(p, TL::by_row(sx, ln, jt, ks), TL::by_row(sy, ln, it, ks));
+                    p = mma_inputs(p, TL::by_row(sx, ln, jt, ks), TL::by_row(sy, ln, it, ks));
                 p *= weights(s, it, jt, i16, g);
                 SC::put(sm, it, jt, p, lane);
 #pragma unroll
@@ -339,13 +339,14 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
     constexpr int NT = DM * 4, NW = DM / 16, KT = DM / 16, KS = DM / 32, IT = Q / 16, QS = Q / 32;
     constexpr int RAW = Parts<T>::raw, MADE = Parts<T>::made, HELD = 3, E = (int)sizeof(T);
     typedef Tile<T, Q, DM, NT, true> TL;
+    typedef Scores<Q, HELD> SU;  // for the gradient of u, which goes into those of the steps as well
     typedef Scores<Q, MADE> SC;
     constexpr int OWN = (SC::TILES + NW - 1) / NW, TURNS = (IT + NW - 1) / NW;
     constexpr bool TWICE = RAW == 3 && DM == 128;
     // one array, so that operands' places differ by constants
-    __shared__ __attribute__((aligned(16))) __bf16 pool[4 * TL::ELEMS + 2 * SC::ELEMS + (TWICE ? 0 : MADE * DM * DM)];
-    __bf16 *const sx = pool, *const sy = sx + TL::ELEMS, *const sb = sy + TL::ELEMS, *const sc = sb + TL::ELEMS, *const sm = sc + TL::ELEMS,
-        *const sg = sm + 2 * SC::ELEMS;  // G [p][n]
+    __shared__ __attribute__((aligned(16))) __bf16 pool[4 * TL::ELEMS + SU::ELEMS + SC::ELEMS + (TWICE ? 0 : MADE * DM * DM)];
+    __bf16 *const sx = pool, *const sy = sx + TL::ELEMS, *const sb = sy + TL::ELEMS, *const sc = sb + TL::ELEMS, *const su = sc + TL::ELEMS,
+        *const sm = su + SU::ELEMS, *const sg = sm + SC::ELEMS;  // sg: G [p][n]
     __shared__ __attribute__((aligned(16))) Steps<Q> ss[2][HB];
     __shared__ float qp[2][NW][Q], xp[2][NW][Q];  // by wave: its columns' part of qint and x . du; of this head and the one before
 
@@ -399,8 +400,8 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
         rct.fetch(rows_at(src.c, left, Q, src.c_bytes), 0);
         rx.fetch(rows_at(src.x, left, Q, src.x_bytes), 0);
         ry.fetch(rows_at(src.y, left, Q, src.y_bytes), 0);
+        SU::clear(su, tid, NT);
         SC::clear(sm, tid, NT);
-        SC::clear(sm + SC::ELEMS, tid, NT);
 #pragma unroll
         for (int k = 0; k < HB; ++k) {
             fetch_dt(0, k);
@@ -480,7 +481,7 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
                     f4 d = (f4)0.0f;
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks)
-                        d = mma(d, TL::by_row(sc, ln, SC::keys(m), ks), TL::by_row(sb, ln, SC::query(m), ks));
+                        d = mma_inputs(d, TL::by_row(sc, ln, SC::keys(m), ks), TL::by_row(sb, ln, SC::query(m), ks));
 #pragma unroll
                     for (int o = 0; o < OWN; ++o)
                         if (o == own) D[o] = d;
@@ -505,7 +506,7 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
                 f4 p = (f4)0.0f, d = D[0];
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks)
-                    p = mma(p, TL::by_row(sy, ln, jt, ks), TL::by_row(sx, ln, it, ks));
+                    p = mma_inputs(p, TL::by_row(sy, ln, jt, ks), TL::by_row(sx, ln, it, ks));
                 if (it == jt) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) skip_sum[k] += 4 * g + r == i16 ? p[r] : 0.0f;
@@ -515,8 +516,8 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
                     if (o == own) d = D[o];
                 ++own;
                 const f4 f = weights(s, it, jt, i16, g);
-                SC::put(sm, it, jt, d * f, lane);
-                SC::put(sm + SC::ELEMS, it, jt, p * (f * s.delta[16 * it + i16]), lane);
+                SU::put(su, it, jt, d * f, lane);
+                SC::put(sm, it, jt, p * (f * s.delta[16 * it + i16]), lane);
             }
             if (w == NW - 1) make_steps<Q, true>(ss[(n + 1) & 1][k], dt[k].value(), bias[k], rate[k], false, lane);
             fetch_dt(n + 2, k);
@@ -579,7 +580,7 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
 #pragma unroll
                 for (int it = 0; it < IT; ++it)
 #pragma unroll
-                    for (int ks = 0; ks <= it / 2; ++ks) O[it] = mma(O[it], vc[ks], SC::get(sm + SC::ELEMS, SC::op(it, ks), lane));
+                    for (int ks = 0; ks <= it / 2; ++ks) O[it] = mma(O[it], vc[ks], SC::get(sm, SC::op(it, ks), lane));
             }
 #pragma unroll
             for (int it = 0; it < IT; ++it) {
@@ -588,7 +589,7 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
                 f4 o = (f4)0.0f;
                 {
 #pragma unroll
-                    for (int ks = 0; ks <= it / 2; ++ks) U[it] = mma(U[it], vy[ks], SC::get(sm, SC::op(it, ks), lane));
+                    for (int ks = 0; ks <= it / 2; ++ks) U[it] = mma(U[it], vy[ks], SU::get(su, SU::op(it, ks), lane));
                     const f4 e = U[it] * xv[it];
                     o = U[it] * s.delta[r] + yv[it] * skip[k];
                     sum = sum_rows(e[0] + e[1] + e[2] + e[3]);

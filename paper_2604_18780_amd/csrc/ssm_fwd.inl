@@ -123,7 +123,7 @@ template <class T, int Q, int DK, int PV, bool OUT, bool REV> __global__ __launc
                 const int it = SC::query(k), jt = SC::keys(k);
                 f4 m = (f4)0.0f;
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) m = mma(m, TK::by_row(sk, lk, jt, ks), q[it][ks]);
+                for (int ks = 0; ks < KS; ++ks) m = mma_inputs(m, TK::by_row(sk, lk, jt, ks), q[it][ks]);
                 m *= weights(s, it, jt, i16, g);
                 if (it == jt) m += skips;
                 SC::put(sm, it, jt, m, lane);

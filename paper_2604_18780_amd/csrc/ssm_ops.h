@@ -63,14 +63,8 @@ template <int n> __device__ __forceinline__ Op<n> split(f8 v)
     return o;
 }
 
-template <int n> __device__ __forceinline__ Op<n> zero_op()
-{
-    Op<n> o;
-#pragma unroll
-    for (int i = 0; i < n; ++i) o.p[i] = (bf8)(__bf16)0.0f;
-    return o;
-}
-
+// Of the products of parts those that matter: the rest is below what the operands' last parts have lost.  Two inputs of two parts
+// each are multiplied out, which is exact.
 template <int na, int nb> __device__ __forceinline__ f4 mma(f4 acc, const Op<na> &a, const Op<nb> &b)
 {
     constexpr int most = na > nb ? na : nb;
@@ -81,68 +75,10 @@ template <int na, int nb> __device__ __forceinline__ f4 mma(f4 acc, const Op<na>
             if (i + j < most) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[j], acc, 0, 0, 0);
     return acc;
 }
-
-// ---- operands from a staged tile ----------------------------------------------------------------------------------
-
-// inner index = column: columns at+4g.., at+16+4g.. of row `row`
-template <class T> __device__ __forceinline__ f8 row_floats(const T *row, int at, int g)
+template <int n> __device__ __forceinline__ f4 mma_inputs(f4 acc, const Op<n> &a, const Op<n> &b)
 {
-    float a[4], b[4];
-    load_n<T, 4>(row + at + 4 * g, a);
-    load_n<T, 4>(row + at + 16 + 4 * g, b);
-    return f8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-}
-template <class T> __device__ __forceinline__ Op<Parts<T>::raw> row_op(const T *row, int at, int g)
-{
-    if constexpr (sizeof(T) == 2 && Parts<T>::raw == 1) {
-        const bf4 a = *(const bf4 *)(row + at + 4 * g), b = *(const bf4 *)(row + at + 16 + 4 * g);
-        Op<1> o;
-        o.p[0] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-        return o;
-    } else {
-        return split<Parts<T>::raw>(row_floats<T>(row, at, g));
-    }
-}
-
-// inner index = row: rows 4g.., 16+4g.. of column `at` + lane % 16
-template <class T, int S> __device__ __forceinline__ void col_raw(const T *tile, int at, int lane, T (&o)[8])
-{
-    const int g = lane >> 4, i = lane & 15;
-    if constexpr (sizeof(T) == 2) {
-        typedef __attribute__((address_space(3))) s4 *lds;
-        T *p = const_cast<T *>(tile) + (4 * g + (i >> 2)) * S + at + 4 * (i & 3);
-        const s4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(p));
-        const s4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(p + 16 * S));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            o[e] = __builtin_bit_cast(T, (short)a[e]);
-            o[4 + e] = __builtin_bit_cast(T, (short)b[e]);
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            o[e] = tile[(4 * g + e) * S + at + i];
-            o[4 + e] = tile[(16 + 4 * g + e) * S + at + i];
-        }
-    }
-}
-template <class T, int S> __device__ __forceinline__ f8 col_floats(const T *tile, int at, int lane)
-{
-    T o[8];
-    col_raw<T, S>(tile, at, lane, o);
-    return f8{(float)o[0], (float)o[1], (float)o[2], (float)o[3], (float)o[4], (float)o[5], (float)o[6], (float)o[7]};
-}
-template <class T, int S> __device__ __forceinline__ Op<Parts<T>::raw> col_op(const T *tile, int at, int lane)
-{
-    if constexpr (sizeof(T) == 2 && Parts<T>::raw == 1) {
-        T o[8];
-        col_raw<T, S>(tile, at, lane, o);
-        Op<1> r;
-        r.p[0] = bf8{o[0], o[1], o[2], o[3], o[4], o[5], o[6], o[7]};
-        return r;
-    } else {
-        return split<Parts<T>::raw>(col_floats<T, S>(tile, at, lane));
-    }
+    if constexpr (n == 2) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[1], b.p[1], acc, 0, 0, 0);
+    return mma(acc, a, b);
 }
 
 }  // namespace semicrf_enc
