@@ -4,20 +4,21 @@
 //   a[t,c] = bias[c] + sum_j w[c,j] u[t-W+1+j,c]        out = a * sigmoid(a)
 //   da = g * silu'(a)     du[t] = sum_k w[W-1-k] da[t+k]     dw[j] = sum_t da[t] u[t-W+1+j]     dbias = sum_t da[t]
 //
-// Bound by memory: every input is read and every output written once (a run's first W-1 tokens twice).  A thread owns 16 bytes
-// of channels and walks RUN positions with the window in registers; sixteen threads side by side make 256-byte rows.
+// Bound by memory: every input is read and every output written once (a run's first W-1 positions twice).  A thread owns 16 bytes
+// of channels and walks a run of positions with the window in registers, the next four rows on their way while four are
+// worked on; sixteen threads side by side make 256-byte rows.
 #include "encoder.h"
 
 namespace semicrf_enc {
 
-constexpr int RUN = 32;
+constexpr uint32_t OUTSIDE = 0x80000000u;  // an offset beyond any range
 
 struct ConvArgs {
     const void *u, *gy, *ring;
     int64_t u_row, gy_row, y_row, gu_row;
     const float *weight, *bias;
     const int32_t *lengths, *seen;
-    int B, T, C, W, runs;
+    int B, T, C, W, run, runs;  // positions of a run (a multiple of 4), runs of a sequence
     unsigned cols;  // workgroups side by side over the channels
     bool linear;
     void *y, *ring_out, *gu;
@@ -44,19 +45,62 @@ template <class T, int W, int V> struct Filter {
     }
 };
 
+// Rows of a run behind one range check: those that lie before the first or behind the sequence's end read as zeros, and a
+// thread's offsets are relative to the first row of its workgroup.
+template <class T> struct RunRows {
+    __amdgpu_buffer_rsrc_t rows;
+    uint32_t first;  // of position 0 of this thread's run
+    int bytes;
+    __device__ __forceinline__ RunRows(const void *p, int64_t row, int64_t block_row, int64_t my_row, int c)
+    {
+        bytes = (int)row * (int)sizeof(T);
+        rows = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>((const char *)p + block_row * bytes), 0, 0x7ffffff0, 0x00020000);
+        first = (uint32_t)((my_row - block_row) * bytes) + (uint32_t)c * (uint32_t)sizeof(T);
+    }
+    __device__ __forceinline__ u4 load(int t, bool in) const
+    {
+        return __builtin_amdgcn_raw_buffer_load_b128(rows, in ? (int)(first + (uint32_t)(t * bytes)) : (int)OUTSIDE, 0, 0);
+    }
+    __device__ __forceinline__ void store(int t, bool in, u4 v) const
+    {
+        __builtin_amdgcn_raw_buffer_store_b128(v, rows, in ? (int)(first + (uint32_t)(t * bytes)) : (int)OUTSIDE, 0, 0);
+    }
+};
+template <class T, int V> __device__ __forceinline__ void widen(u4 r, float (&o)[V])
+{
+    typedef T X __attribute__((ext_vector_type(V)));
+    const X v = __builtin_bit_cast(X, r);
+#pragma unroll
+    for (int e = 0; e < V; ++e) o[e] = (float)v[e];
+}
+template <class T, int V> __device__ __forceinline__ u4 narrow(const float (&o)[V])
+{
+    typedef T X __attribute__((ext_vector_type(V)));
+    typedef float F __attribute__((ext_vector_type(V)));
+    F f;
+#pragma unroll
+    for (int e = 0; e < V; ++e) f[e] = o[e];
+    return __builtin_bit_cast(u4, __builtin_convertvector(f, X));
+}
+
 template <class T, int W> __global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs a)
 {
     constexpr int V = PER16<T>;
     const int c = (int)(blockIdx.x % a.cols * 16 + threadIdx.x % 16) * V;
-    const int64_t id = (int64_t)(blockIdx.x / a.cols) * 16 + threadIdx.x / 16;
+    const int64_t id0 = (int64_t)(blockIdx.x / a.cols) * 16, id = id0 + threadIdx.x / 16;
     if (c >= a.C || id >= (int64_t)a.B * a.runs) return;
-    const int b = (int)(id / a.runs), t0 = (int)(id % a.runs) * RUN;
+    const int b = (int)(id / a.runs), t0 = (int)(id % a.runs) * a.run;
+    const int64_t row0 = id0 / a.runs * a.T + id0 % a.runs * a.run, row = (int64_t)b * a.T + t0;
     const int seen = a.seen ? a.seen[b] : 0, L = seen < 0 ? 0 : length_of(a.lengths, b, a.T);
     const T *u = (const T *)a.u + (int64_t)b * a.T * a.u_row + c;
-    T *y = (T *)a.y + (int64_t)b * a.T * a.y_row + c;
+    const RunRows<T> in(a.u, a.u_row, row0, row, c), out(a.y, a.y_row, row0, row, c);
+    const T *ring = a.ring ? (const T *)a.ring + ((int64_t)b * a.C + c) * W : nullptr;
+    const int n = t0 + a.run < a.T ? a.run : a.T - t0, have = L - t0;  // rows to write, rows that exist
+    u4 next[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) next[k] = in.load(k, k < have);
     const Filter<T, W, V> f(a, c);
     float win[W][V];  // win[j]: position t - W + 1 + j
-    const T *ring = a.ring ? (const T *)a.ring + ((int64_t)b * a.C + c) * W : nullptr;
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) {
         const int t = t0 - W + 1 + j;
@@ -69,27 +113,30 @@ template <class T, int W> __global__ __launch_bounds__(256) void k_conv_fwd(Conv
             for (int e = 0; e < V; ++e) win[j + 1][e] = (float)ring[(int64_t)e * W + (seen + t) % W];
         }
     }
-    const int t1 = t0 + RUN < a.T ? t0 + RUN : a.T;
-    for (int t = t0; t < t1; ++t) {
-        float o[V];
+    for (int t = 0; t < n; t += 4) {
+        u4 now[4];
 #pragma unroll
-        for (int j = 0; j < W - 1; ++j)
+        for (int k = 0; k < 4; ++k) now[k] = next[k];
 #pragma unroll
-            for (int e = 0; e < V; ++e) win[j][e] = win[j + 1][e];
-        if (t < L) {
-            load_n<T, V>(u + t * a.u_row, win[W - 1]);
+        for (int k = 0; k < 4; ++k) next[k] = in.load(t + 4 + k, t + 4 + k < have && t + 4 < n);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float o[V];
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+                for (int e = 0; e < V; ++e) win[j][e] = win[j + 1][e];
+            widen<T, V>(now[k], win[W - 1]);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                o[e] = f.b[e];
+                float v = f.b[e];
 #pragma unroll
-                for (int j = 0; j < W; ++j) o[e] += f.w[j][e] * win[j][e];
-                if (!a.linear) o[e] *= fast_sigmoid(o[e]);
+                for (int j = 0; j < W; ++j) v += f.w[j][e] * win[j][e];
+                if (!a.linear) v *= fast_sigmoid(v);
+                o[e] = t + k < have ? v : 0.0f;
             }
-        } else {
-#pragma unroll
-            for (int e = 0; e < V; ++e) o[e] = 0.0f;
+            out.store(t + k, t + k < n, narrow<T, V>(o));
         }
-        store_n<T, V>(y + t * a.y_row, o);
     }
     if (t0 == 0 && a.ring_out) {
         // the last W tokens, each at its position modulo W; this thread alone touches these channels' ring
@@ -129,56 +176,69 @@ template <class T, int W> __global__ __launch_bounds__(256) void k_conv_bwd(Conv
     if (c < a.C) {
         const Filter<T, W, V> f(a, c);
         for (int64_t id = block * 16 + threadIdx.x / 16; id < (int64_t)a.B * a.runs; id += (int64_t)a.blocks * 16) {
-            const int b = (int)(id / a.runs), t0 = (int)(id % a.runs) * RUN;
+            const int b = (int)(id / a.runs), t0 = (int)(id % a.runs) * a.run;
+            const int64_t id0 = id - threadIdx.x / 16;
+            const int64_t row0 = id0 / a.runs * a.T + id0 % a.runs * a.run, row = (int64_t)b * a.T + t0;
             const int L = length_of(a.lengths, b, a.T);
-            const T *u = (const T *)a.u + (int64_t)b * a.T * a.u_row + c;
-            const T *gy = (const T *)a.gy + (int64_t)b * a.T * a.gy_row + c;
-            T *gu = (T *)a.gu + (int64_t)b * a.T * a.gu_row + c;
-            const int t1 = t0 + RUN < a.T ? t0 + RUN : a.T;
+            const RunRows<T> in(a.u, a.u_row, row0, row, c), gin(a.gy, a.gy_row, row0, row, c), out(a.gu, a.gu_row, row0, row, c);
+            const int n = t0 + a.run < a.T ? a.run : a.T - t0, have = L - t0;
+            u4 nu[4], ng[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) nu[k] = in.load(k, k < have), ng[k] = gin.load(k, k < have);
             float win[W][V], da[W][V];
 #pragma unroll
             for (int j = 0; j < W; ++j)
 #pragma unroll
                 for (int e = 0; e < V; ++e) win[j][e] = da[j][e] = 0.0f;
+            const T *u = (const T *)a.u + (int64_t)b * a.T * a.u_row + c;
 #pragma unroll
             for (int j = 0; j < W - 1; ++j) {
                 const int t = t0 - W + 1 + j;
                 if (t >= 0 && t < L) load_n<T, V>(u + t * a.u_row, win[j + 1]);
             }
-            for (int t = t0; t < t1 + W - 1; ++t) {
+            // a gradient of u needs the W-1 positions behind it: rows n .. n+W-2 are looked at, and counted by the run they are in
+            for (int t = 0; t < n + W - 1; t += 4) {
+                u4 uu[4], gg[4];
 #pragma unroll
-                for (int j = 0; j < W - 1; ++j)
+                for (int k = 0; k < 4; ++k) uu[k] = nu[k], gg[k] = ng[k];
 #pragma unroll
-                    for (int e = 0; e < V; ++e) win[j][e] = win[j + 1][e], da[j][e] = da[j + 1][e];
-                float g[V];
-                const bool in = t < L;
-                if (in) {
-                    load_n<T, V>(u + t * a.u_row, win[W - 1]);
-                    load_n<T, V>(gy + t * a.gy_row, g);
+                for (int k = 0; k < 4; ++k) {
+                    const bool want = t + 4 + k < have && t + 4 < n + W - 1;
+                    nu[k] = in.load(t + 4 + k, want), ng[k] = gin.load(t + 4 + k, want);
                 }
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    float v = f.b[e];
+                for (int k = 0; k < 4; ++k) {
+                    float g[V];
 #pragma unroll
-                    for (int j = 0; j < W; ++j) v += f.w[j][e] * win[j][e];
-                    const float s = fast_sigmoid(v);
-                    da[W - 1][e] = in ? (a.linear ? g[e] : g[e] * s * (1.0f + v * (1.0f - s))) : 0.0f;
-                    if (t < t1 && in) {
+                    for (int j = 0; j < W - 1; ++j)
 #pragma unroll
-                        for (int j = 0; j < W; ++j) dw[j][e] += da[W - 1][e] * win[j][e];
-                        dw[W][e] += da[W - 1][e];
+                        for (int e = 0; e < V; ++e) win[j][e] = win[j + 1][e], da[j][e] = da[j + 1][e];
+                    widen<T, V>(uu[k], win[W - 1]);
+                    widen<T, V>(gg[k], g);
+                    // rows that do not exist have g = 0, and so no share in anything
+                    const float mine = t + k < n ? 1.0f : 0.0f;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        float v = f.b[e];
+#pragma unroll
+                        for (int j = 0; j < W; ++j) v += f.w[j][e] * win[j][e];
+                        const float s = fast_sigmoid(v);
+                        const float d = a.linear ? g[e] : g[e] * s * (1.0f + v * (1.0f - s));
+                        da[W - 1][e] = d;
+                        const float m = d * mine;
+#pragma unroll
+                        for (int j = 0; j < W; ++j) dw[j][e] += m * win[j][e];
+                        dw[W][e] += m;
                     }
-                }
-                const int to = t - W + 1;
-                if (to >= t0) {
                     float o[V];
 #pragma unroll
                     for (int e = 0; e < V; ++e) {
                         o[e] = 0.0f;
 #pragma unroll
-                        for (int k = 0; k < W; ++k) o[e] += f.w[W - 1 - k][e] * da[k][e];
+                        for (int j = 0; j < W; ++j) o[e] += f.w[W - 1 - j][e] * da[j][e];
                     }
-                    store_n<T, V>(gu + to * a.gu_row, o);
+                    const int to = t + k - (W - 1);
+                    out.store(to, to >= 0 && to < n, narrow<T, V>(o));
                 }
             }
         }
@@ -221,14 +281,25 @@ __global__ __launch_bounds__(256) void k_conv_params(ConvArgs a)
 int conv_sizes(int B, int T, int C, int W)
 {
     if (B < 1 || T < 1 || C < 1 || W < 1) return SEMICRF_EINVAL;
-    if (C % 8 || W > 4 || T > (1 << 30) || (double)B * ((T + RUN - 1) / RUN) * (C / 4) > 2e9) return SEMICRF_EUNSUPPORTED;
+    if (C % 8 || W > 4 || T > (1 << 30) || (double)B * ((T + 7) / 8) * (C / 4) > 2e9) return SEMICRF_EUNSUPPORTED;
     return SEMICRF_OK;
+}
+
+// Positions of a run: 32, so that the W-1 positions read twice are a tenth, but as few as 8 where that leaves the chip (256
+// compute units of 2048 threads) less than half filled.
+int run_length(int B, int T, int C, int per16)
+{
+    const int64_t threads = (int64_t)B * T * (C / per16);
+    int run = 32;
+    while (run > 8 && threads / run < 256 * 1024) run /= 2;
+    return run;
 }
 
 // Workgroups along the sequences in a backward call: two thousand in all keep the chip busy, and each leaves a row of sums.
 int conv_blocks(int B, int T, int C, int per16)
 {
-    const int64_t runs = (int64_t)B * ((T + RUN - 1) / RUN), cols = (C / per16 + 15) / 16;
+    const int run = run_length(B, T, C, per16);
+    const int64_t runs = (int64_t)B * ((T + run - 1) / run), cols = (C / per16 + 15) / 16;
     int64_t n = (runs + 15) / 16, most = 2048 / cols + 1;
     return (int)(n < most ? n : most);
 }
@@ -267,11 +338,12 @@ int semicrf_conv_fwd(const void *u, int64_t u_row, const float *weight, const fl
 {
     if (int rc = conv_sizes(B, T, C, W)) return rc;
     const int type = act_type(flags);
-    if (type < 0 || !weight || (ring && !seen) || !rows_ok(u, u_row, C, type) || !rows_ok(out, out_row, C, type))
+    if (type < 0 || !weight || (ring && !seen) || u_row > (1 << 19) || out_row > (1 << 19) || !rows_ok(u, u_row, C, type) || !rows_ok(out, out_row, C, type))
         return SEMICRF_EINVAL;
     ConvArgs a = {};
     a.u = u; a.u_row = u_row; a.weight = weight; a.bias = bias; a.lengths = lengths; a.seen = seen; a.ring = ring;
-    a.B = B; a.T = T; a.C = C; a.W = W; a.runs = (T + RUN - 1) / RUN;
+    a.B = B; a.T = T; a.C = C; a.W = W; a.run = run_length(B, T, C, 16 / act_bytes(type));
+    a.runs = (T + a.run - 1) / a.run;
     a.linear = (flags & SEMICRF_CONV_LINEAR) != 0;
     a.y = out; a.y_row = out_row; a.ring_out = ring_out;
     return conv_run(a, type, false, (hipStream_t)stream);
@@ -281,7 +353,10 @@ int semicrf_conv_bwd_workspace_bytes(int B, int T, int C, int W, size_t *bytes)
 {
     if (!bytes) return SEMICRF_EINVAL;
     const int rc = conv_sizes(B, T, C, W);
-    if (rc == SEMICRF_OK) *bytes = align256((size_t)conv_blocks(B, T, C, 8) * C * (W + 1) * 4);
+    if (rc == SEMICRF_OK) {
+        const int a = conv_blocks(B, T, C, 4), b = conv_blocks(B, T, C, 8);
+        *bytes = align256((size_t)(a > b ? a : b) * C * (W + 1) * 4);
+    }
     return rc;
 }
 
@@ -293,14 +368,15 @@ int semicrf_conv_bwd(const void *u, int64_t u_row, const float *weight, const fl
     size_t need = 0;
     if (int rc = semicrf_conv_bwd_workspace_bytes(B, T, C, W, &need)) return rc;
     const int type = act_type(flags);
-    if (type < 0 || !weight || !grad_weight || !rows_ok(u, u_row, C, type) ||
+    if (type < 0 || !weight || !grad_weight || u_row > (1 << 19) || grad_out_row > (1 << 19) || grad_u_row > (1 << 19) || !rows_ok(u, u_row, C, type) ||
         !rows_ok(grad_out, grad_out_row, C, type) || !rows_ok(grad_u, grad_u_row, C, type))
         return SEMICRF_EINVAL;
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need) return SEMICRF_EWORKSPACE;
     ConvArgs a = {};
     a.u = u; a.u_row = u_row; a.weight = weight; a.bias = bias; a.lengths = lengths;
     a.gy = grad_out; a.gy_row = grad_out_row; a.gu = grad_u; a.gu_row = grad_u_row;
-    a.B = B; a.T = T; a.C = C; a.W = W; a.runs = (T + RUN - 1) / RUN;
+    a.B = B; a.T = T; a.C = C; a.W = W; a.run = run_length(B, T, C, 16 / act_bytes(type));
+    a.runs = (T + a.run - 1) / a.run;
     a.linear = (flags & SEMICRF_CONV_LINEAR) != 0;
     a.part = (float *)workspace; a.gw = grad_weight; a.gb = grad_bias;
     a.blocks = conv_blocks(B, T, C, act_bytes(type) == 4 ? 4 : 8);

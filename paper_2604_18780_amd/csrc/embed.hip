@@ -5,45 +5,58 @@
 // The gradient has no atomics: positions are sorted by token (stable radix sort, 8 bits a pass), and rows are added up in that
 // order, in 32 bits.  Texts are skewed, so the sorted positions are cut into chunks of equal length instead of one piece of work
 // for each token: a chunk writes the tokens that lie in it whole, and leaves a partial row where one enters from the chunk
-// before or goes on in the next; those are joined in chunk order.  Bound by g read once and the table written once.
+// before or goes on in the next; those are joined in chunk order.  Zeros for tokens that do not occur are written while the
+// positions are sorted, which keeps few workgroups busy.  Bound by g read once and the table written once; for few tokens by the
+// launches: three a pass and two.
 #include "encoder.h"
 
 namespace semicrf_enc {
 
-constexpr int TILE = 2048;     // positions a workgroup sorts at once
 constexpr int RADIX = 256;
 
 struct EmbedArgs {
     const int32_t *tokens, *lengths;
     const void *table, *g;
     float scale;
-    int B, T, V, D;
+    int B, T, V, D, lanes;  // lanes of a row in k_embed_fwd, as a power of two
     void *out;
     float *grad;
-    int n, tiles, chunk, chunks;
-    uint32_t *key[2], *pos[2], *count, *start;
+    int n, tiles, chunk, chunks, fills;  // fills: launches that share the zeros
+    uint32_t *key[2], *pos[2], *count, *digit;
     float *part;  // [chunks][2][D]
 };
 
+// A row is 16 bytes a lane over a power of two of lanes (some idle where a row is none), four rows to a lane at once; a workgroup
+// stays within one sequence, so that no position is divided by anything.
+constexpr int ROWS = 4;
 template <class T> __global__ __launch_bounds__(256) void k_embed_fwd(EmbedArgs a)
 {
     constexpr int E = PER16<T>;
-    const int per = a.D / E;
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= (int64_t)a.n * per) return;
-    const int64_t row = at / per;
-    const int col = (int)(at % per) * E, b = (int)(row / a.T), t = (int)(row % a.T);
-    const int32_t v = a.tokens[row];
-    float o[E];
-    if (t < length_of(a.lengths, b, a.T) && v >= 0 && v < a.V) {
-        load_n<T, E>((const T *)a.table + (int64_t)v * a.D + col, o);
+    typedef T X __attribute__((ext_vector_type(E)));
+    const int side = 256 >> a.lanes, tiles = (a.T + ROWS * side - 1) / (ROWS * side);  // rows side by side in a workgroup
+    const int b = blockIdx.x / tiles, t0 = blockIdx.x % tiles * (ROWS * side) + (threadIdx.x >> a.lanes);
+    const int L = length_of(a.lengths, b, a.T), first = (threadIdx.x & ((1 << a.lanes) - 1)) * E;
+    int32_t v[ROWS];
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] *= a.scale;
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = 0.0f;
+    for (int k = 0; k < ROWS; ++k) {
+        const int t = t0 + k * side;
+        v[k] = t < L ? a.tokens[(int64_t)b * a.T + t] : -1;
     }
-    store_n<T, E>((T *)a.out + row * a.D + col, o);
+    for (int col = first; col < a.D; col += E << a.lanes) {
+        X x[ROWS];
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            x[k] = (X)(T)0.0f;
+            if (v[k] >= 0 && v[k] < a.V) x[k] = *(const X *)((const T *)a.table + (int64_t)v[k] * a.D + col);
+        }
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            X o;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = (T)((float)x[k][e] * (v[k] >= 0 && v[k] < a.V ? a.scale : 0.0f));
+            if (t0 + k * side < a.T) __builtin_nontemporal_store(o, (X *)((T *)a.out + ((int64_t)b * a.T + t0 + k * side) * a.D + col));
+        }
+    }
 }
 
 // The key of position i: its token, or V where it holds none (sorted to the end, never added).
@@ -54,63 +67,87 @@ __device__ __forceinline__ uint32_t key_of(const EmbedArgs &a, int i)
     return t < length_of(a.lengths, b, a.T) && v >= 0 && v < a.V ? (uint32_t)v : (uint32_t)a.V;
 }
 
-// How often each digit occurs in each tile: count[digit][tile].
-__global__ __launch_bounds__(256) void k_sort_count(EmbedArgs a, int shift)
+// The workgroups of a sorting launch beyond its tiles clear a share of the gradient.
+constexpr int CLEAR = 512;
+__device__ __forceinline__ bool clear_share(const EmbedArgs &a, int launch)
+{
+    if ((int)blockIdx.x < a.tiles) return false;
+    const int64_t all = (int64_t)a.V * a.D / 4, from = all * launch / a.fills, to = all * (launch + 1) / a.fills;
+    for (int64_t k = from + (int64_t)(blockIdx.x - a.tiles) * 256 + threadIdx.x; k < to; k += CLEAR * 256) *(f4 *)(a.grad + 4 * k) = (f4)0.0f;
+    return true;
+}
+
+// How often each digit occurs in each tile of 256 * ROUNDS positions: count[digit][tile].
+template <int ROUNDS> __global__ __launch_bounds__(256) void k_sort_count(EmbedArgs a, int shift)
 {
     __shared__ uint32_t c[RADIX];
+    if (clear_share(a, shift / 4)) return;
     c[threadIdx.x] = 0;
     __syncthreads();
-    const int first = blockIdx.x * TILE;
-    for (int k = threadIdx.x; k < TILE && first + k < a.n; k += 256) {
-        const uint32_t key = shift ? a.key[(shift / 8) & 1][first + k] : key_of(a, first + k);
-        atomicAdd(&c[(key >> shift) % RADIX], 1u);
-    }
+    const int first = blockIdx.x * 256 * ROUNDS + threadIdx.x;
+    uint32_t key[ROUNDS];
+#pragma unroll
+    for (int k = 0; k < ROUNDS; ++k)
+        if (first + 256 * k < a.n) key[k] = shift ? a.key[(shift / 8) & 1][first + 256 * k] : key_of(a, first + 256 * k);
+#pragma unroll
+    for (int k = 0; k < ROUNDS; ++k)
+        if (first + 256 * k < a.n) atomicAdd(&c[(key[k] >> shift) % RADIX], 1u);
     __syncthreads();
     a.count[threadIdx.x * a.tiles + blockIdx.x] = c[threadIdx.x];
 }
 
-// Exclusive prefix sum over the counts, digits outside, tiles inside.  One workgroup.
-__global__ __launch_bounds__(1024) void k_sort_offsets(EmbedArgs a)
+// Prefix sum of a wave's values, exclusive; `all` is their sum.
+__device__ __forceinline__ uint32_t before_lane(uint32_t v, uint32_t &all)
 {
-    __shared__ uint32_t wave[16];
-    const int n = RADIX * a.tiles, per = (n + 1023) / 1024, first = threadIdx.x * per;
-    const int lane = threadIdx.x % 64, w = threadIdx.x / 64;
-    uint32_t sum = 0;
-    for (int k = 0; k < per; ++k)
-        if (first + k < n) sum += a.count[first + k];
-    uint32_t run = sum;
+    uint32_t run = v;
+#pragma unroll
     for (int d = 1; d < 64; d *= 2) {
         const uint32_t o = __shfl_up(run, d);
-        if (lane >= d) run += o;
+        if ((int)(threadIdx.x & 63) >= d) run += o;
     }
-    if (lane == 63) wave[w] = run;
-    __syncthreads();
-    uint32_t base = run - sum;
-    for (int k = 0; k < w; ++k) base += wave[k];
-    for (int k = 0; k < per; ++k)
-        if (first + k < n) {
-            const uint32_t c = a.count[first + k];
-            a.count[first + k] = base;
-            base += c;
-        }
+    all = __shfl(run, 63);
+    return run - v;
 }
 
-// Puts a tile's positions in their places.  A wave takes 64 positions at a time, in order; its place among equal digits is
-// what earlier waves, earlier rounds and lower lanes hold, so equal keys keep their order.
-__global__ __launch_bounds__(256) void k_sort_scatter(EmbedArgs a, int shift)
+// For each digit, what earlier tiles hold of it, and how often it occurs in all.  One wave to a digit.
+__global__ __launch_bounds__(64) void k_sort_offsets(EmbedArgs a)
 {
-    constexpr int ROUNDS = TILE / 256;
-    __shared__ uint32_t c[4][RADIX];
+    uint32_t base = 0, all;
+    for (int k = threadIdx.x; k - (int)threadIdx.x < a.tiles; k += 64) {
+        uint32_t *c = a.count + (size_t)blockIdx.x * a.tiles + k;
+        const uint32_t v = k < a.tiles ? *c : 0, at = base + before_lane(v, all);
+        if (k < a.tiles) *c = at;
+        base += all;
+    }
+    if (threadIdx.x == 0) a.digit[blockIdx.x] = base;
+}
+
+// Puts a tile's positions in their places.  A wave takes 64 positions at a time, in order; a position's place among equal digits
+// is what earlier tiles, waves, rounds and lower lanes hold, so equal keys keep their order.
+template <int ROUNDS> __global__ __launch_bounds__(256) void k_sort_scatter(EmbedArgs a, int shift)
+{
+    __shared__ uint32_t c[4][RADIX], wave[4];
+    if (clear_share(a, shift / 4 + 1)) return;
     const int lane = threadIdx.x % 64, w = threadIdx.x / 64, pass = shift / 8;
     for (int k = 0; k < 4; ++k) c[k][threadIdx.x] = 0;
-    __syncthreads();
-    const int first = blockIdx.x * TILE + w * (TILE / 4);
-    uint32_t key[ROUNDS], rank[ROUNDS];
+    const uint32_t earlier = a.count[threadIdx.x * a.tiles + blockIdx.x], here = a.digit[threadIdx.x];
+    uint32_t all;
+    uint32_t base = before_lane(here, all);
+    if (lane == 63) wave[w] = all;
+    const int first = blockIdx.x * 256 * ROUNDS + w * 64 * ROUNDS + lane;
+    uint32_t key[ROUNDS], pos[ROUNDS], rank[ROUNDS];
 #pragma unroll
     for (int k = 0; k < ROUNDS; ++k) {
-        const int i = first + 64 * k + lane;
-        const bool in = i < a.n;
-        key[k] = !in ? 0 : pass ? a.key[pass & 1][i] : key_of(a, i);
+        const int i = first + 64 * k;
+        key[k] = i >= a.n ? 0 : pass ? a.key[pass & 1][i] : key_of(a, i);
+        pos[k] = i >= a.n ? 0 : pass ? a.pos[pass & 1][i] : (uint32_t)i;
+    }
+    __syncthreads();
+    for (int k = 0; k < w; ++k) base += wave[k];
+    base += earlier;
+#pragma unroll
+    for (int k = 0; k < ROUNDS; ++k) {
+        const bool in = first + 64 * k < a.n;
         const uint32_t d = (key[k] >> shift) % RADIX;
         uint64_t same = __ballot(in);
 #pragma unroll
@@ -127,97 +164,126 @@ __global__ __launch_bounds__(256) void k_sort_scatter(EmbedArgs a, int shift)
         __builtin_amdgcn_wave_barrier();
     }
     __syncthreads();
-    {
-        uint32_t base = a.count[threadIdx.x * a.tiles + blockIdx.x];
-        for (int k = 0; k < 4; ++k) {
-            const uint32_t n = c[k][threadIdx.x];
-            c[k][threadIdx.x] = base;
-            base += n;
-        }
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t n = c[k][threadIdx.x];
+        c[k][threadIdx.x] = base;
+        base += n;
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < ROUNDS; ++k) {
-        const int i = first + 64 * k + lane;
-        if (i < a.n) {
+    for (int k = 0; k < ROUNDS; ++k)
+        if (first + 64 * k < a.n) {
             const uint32_t to = c[w][(key[k] >> shift) % RADIX] + rank[k];
             a.key[(pass + 1) & 1][to] = key[k];
-            a.pos[(pass + 1) & 1][to] = pass ? a.pos[pass & 1][i] : (uint32_t)i;
+            a.pos[(pass + 1) & 1][to] = pos[k];
         }
-    }
 }
 
-// First sorted place of each token, by bisection; place V is where the positions without a token begin.
-__global__ __launch_bounds__(256) void k_embed_starts(EmbedArgs a, const uint32_t *key)
-{
-    const int v = blockIdx.x * 256 + threadIdx.x;
-    if (v > a.V) return;
-    int lo = 0, hi = a.n;
-    while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (key[mid] < (uint32_t)v) lo = mid + 1;
-        else hi = mid;
-    }
-    a.start[v] = lo;
-}
-
-// One wave adds up one chunk of the sorted positions over 64 lanes of columns.
+// One wave adds up one chunk of the sorted positions over 64 lanes of columns.  Keys and places are a lane's each, read once and
+// handed round by lane, so that branches on them are the wave's and the rows of several positions are on their way at once.
 template <class T> __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs a, const uint32_t *key, const uint32_t *pos)
 {
-    constexpr int E = PER16<T>;
-    const int slices = (a.D + 64 * E - 1) / (64 * E);
-    const int id = blockIdx.x * 4 + threadIdx.x / 64, chunk = id / slices;
-    const int col = (id % slices * 64 + threadIdx.x % 64) * E;
-    const int end = (int)a.start[a.V];
-    const int first = chunk * a.chunk;
-    if (chunk >= a.chunks || first >= end || col >= a.D) return;
-    const int last = first + a.chunk < end ? first + a.chunk : end;
-    const T *g = (const T *)a.g + col;
+    constexpr int E = PER16<T>, AHEAD = 8;
+    typedef T X __attribute__((ext_vector_type(E)));
+    const int slices = (a.D + 64 * E - 1) / (64 * E), lane = threadIdx.x % 64;
+    const int id = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / 64), chunk = id / slices;
+    const int col = (id % slices * 64 + lane) * E, first = chunk * a.chunk;
+    if (chunk >= a.chunks) return;
+    const int n = first + a.chunk < a.n ? a.chunk : a.n - first;
+    const uint32_t mine = lane < n ? key[first + lane] : ~0u, at = lane < n ? pos[first + lane] : 0;
+    const uint32_t last = first + n < a.n ? key[first + n] : ~0u;  // the key behind the chunk
+    uint32_t run = first > 0 ? key[first - 1] : ~0u;
+    const bool here = col < a.D;
+    const T *g = (const T *)a.g + (here ? col : 0);
     float s[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) s[e] = 0.0f;
-    bool entered = first > 0 && key[first - 1] == key[first];
-    for (int i = first; i < last; ++i) {
-        const uint32_t v = key[i];
-        float r[E];
-        load_n<T, E>(g + (int64_t)pos[i] * a.D, r);
+    bool entered = run == (uint32_t)__builtin_amdgcn_readlane((int)mine, 0);
+    X next[AHEAD];
+    auto fetch = [&](int i0) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) s[e] += r[e];
-        const bool ends = i + 1 == end || key[i + 1] != v;
-        if (ends || i + 1 == last) {
-            float *to = entered ? a.part + ((int64_t)chunk * 2) * a.D + col
-                                : ends ? a.grad + (int64_t)v * a.D + col : a.part + ((int64_t)chunk * 2 + 1) * a.D + col;
-            const float f = entered || !ends ? 1.0f : a.scale;
+        for (int k = 0; k < AHEAD; ++k) {
+            const int i = i0 + k < n ? i0 + k : n - 1;
+            next[k] = *(const X *)(g + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)at, i) * a.D);
+        }
+    };
+    fetch(0);
+    for (int i0 = 0; i0 < n; i0 += AHEAD) {
+        X r[AHEAD];
 #pragma unroll
-            for (int e = 0; e < E; ++e) to[e] = f * s[e], s[e] = 0.0f;
-            entered = false;
+        for (int k = 0; k < AHEAD; ++k) r[k] = next[k];
+        if (i0 + AHEAD < n) fetch(i0 + AHEAD);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int i = i0 + k;
+            if (i >= n) break;
+            const uint32_t v = (uint32_t)__builtin_amdgcn_readlane((int)mine, i);
+            if (v >= (uint32_t)a.V) return;  // positions without a token are the last
+#pragma unroll
+            for (int e = 0; e < E; ++e) s[e] += (float)r[k][e];
+            const bool ends = (i + 1 < n ? (uint32_t)__builtin_amdgcn_readlane((int)mine, i + 1) : last) != v;
+            if (ends || i + 1 == n) {
+                float *to = entered ? a.part + ((int64_t)chunk * 2) * a.D + col
+                                    : ends ? a.grad + (int64_t)v * a.D + col : a.part + ((int64_t)chunk * 2 + 1) * a.D + col;
+                const float f = entered || !ends ? 1.0f : a.scale;
+#pragma unroll
+                for (int e = 0; e < E; ++e) s[e] *= f;
+                if (here) {
+#pragma unroll
+                    for (int q = 0; q < E; q += 4) *(f4 *)(to + q) = (f4){s[q], s[q + 1], s[q + 2], s[q + 3]};
+                }
+#pragma unroll
+                for (int e = 0; e < E; ++e) s[e] = 0.0f;
+                entered = false;
+            }
         }
     }
 }
 
-// Tokens that no chunk held whole: zeros where there are none, else the parts in chunk order.  256 threads to a token and 256
-// columns.
-__global__ __launch_bounds__(256) void k_embed_join(EmbedArgs a)
+// Tokens that no chunk held whole: the chunk that such a token's positions end in adds up its parts, in chunk order.
+__global__ __launch_bounds__(256) void k_embed_join(EmbedArgs a, const uint32_t *key)
 {
-    const int slices = (a.D + 255) / 256, v = blockIdx.x / slices, col = blockIdx.x % slices * 256 + threadIdx.x;
-    if (col >= a.D) return;
-    const int s = (int)a.start[v], e = (int)a.start[v + 1];
-    float *to = a.grad + (int64_t)v * a.D + col;
-    if (s == e) {
-        *to = 0.0f;
-        return;
+    const int lane = threadIdx.x % 64, chunk = blockIdx.x * 4 + threadIdx.x / 64, first = chunk * a.chunk;
+    if (chunk < 1 || chunk >= a.chunks) return;
+    const uint32_t v = key[first];
+    const int end = first + a.chunk < a.n ? first + a.chunk : a.n;
+    if (v >= (uint32_t)a.V || key[first - 1] != v) return;
+    if (key[end - 1] == v && end < a.n && key[end] == v) return;  // goes on in the next chunk
+    // the token's first position, 64 probes at a time: lo is at or before it, hi behind the last that may be
+    int lo = 0, hi = first;
+    while (lo < hi) {
+        const int step = (hi - lo + 63) / 64, at = lo + lane * step;
+        const int less = __popcll(__ballot(at < hi && key[at] < v));  // the first `less` probes lie before it
+        if (less == 0) {
+            hi = lo;
+        } else {
+            const int up = lo + less * step;
+            lo += (less - 1) * step + 1;
+            hi = up < hi ? up : hi;
+        }
     }
-    const int c0 = s / a.chunk, c1 = (e - 1) / a.chunk;
-    if (c0 == c1) return;
-    const float *part = a.part + col;
-    double sum = part[((int64_t)c0 * 2 + 1) * a.D];
-    for (int c = c0 + 1; c <= c1; ++c) sum += part[(int64_t)c * 2 * a.D];
-    *to = (float)(a.scale * sum);
+    const int c0 = lo / a.chunk;
+    for (int col = 4 * lane; col < a.D; col += 256) {
+        const float *part = a.part + col;
+        typedef double d4 __attribute__((ext_vector_type(4)));
+        d4 sum = __builtin_convertvector(*(const f4 *)(part + ((int64_t)c0 * 2 + 1) * a.D), d4);
+        int c = c0 + 1;
+        for (; c + 8 <= chunk + 1; c += 8) {
+            f4 p[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) p[q] = *(const f4 *)(part + (int64_t)(c + q) * 2 * a.D);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) sum += __builtin_convertvector(p[q], d4);
+        }
+        for (; c <= chunk; ++c) sum += __builtin_convertvector(*(const f4 *)(part + (int64_t)c * 2 * a.D), d4);
+        *(f4 *)(a.grad + (int64_t)v * a.D + col) = __builtin_convertvector(sum * (double)a.scale, f4);
+    }
 }
 
 struct EmbedPlan {
     int n, tiles, chunk, chunks, passes;
-    size_t key[2], pos[2], count, start, part, total;
+    bool large;
+    size_t key[2], pos[2], count, digit, part, total;
 };
 
 int embed_plan(int B, int T, int V, int D, EmbedPlan *p)
@@ -225,7 +291,10 @@ int embed_plan(int B, int T, int V, int D, EmbedPlan *p)
     if (B < 1 || T < 1 || V < 1 || D < 1) return SEMICRF_EINVAL;
     if (D % 8 || (double)B * T > 1e9 || V > (1 << 24) || (double)V * D > 1e11) return SEMICRF_EUNSUPPORTED;
     p->n = B * T;
-    p->tiles = (p->n + TILE - 1) / TILE;
+    // Tiles of 2048 positions, or of 512 where few would leave most of the chip idle (64 x 256 tokens: 9 us a pass, 16 with 2048);
+    // chunks of 64, or of 16 for the same reason.
+    p->large = p->n > 131072;
+    p->tiles = (p->n + (p->large ? 2047 : 511)) / (p->large ? 2048 : 512);
     p->chunk = p->n > 262144 ? 64 : 16;
     p->chunks = (p->n + p->chunk - 1) / p->chunk;
     p->passes = 0;
@@ -238,7 +307,7 @@ int embed_plan(int B, int T, int V, int D, EmbedPlan *p)
     };
     for (int k = 0; k < 2; ++k) p->key[k] = take((size_t)p->n * 4), p->pos[k] = take((size_t)p->n * 4);
     p->count = take((size_t)RADIX * p->tiles * 4);
-    p->start = take(((size_t)V + 1) * 4);
+    p->digit = take((size_t)RADIX * 4);
     p->part = take((size_t)p->chunks * 2 * D * 4);
     p->total = at;
     return SEMICRF_OK;
@@ -266,9 +335,10 @@ int semicrf_embed_fwd(const int32_t *tokens, const int32_t *lengths, const void 
     EmbedArgs a = {};
     a.tokens = tokens; a.lengths = lengths; a.table = table; a.scale = scale;
     a.B = B; a.T = T; a.V = V; a.D = D; a.out = out; a.n = p.n;
-    const int64_t items = (int64_t)p.n * (D / (16 / act_bytes(type)));
-    if (items > (int64_t)0x7fffffff * 256) return SEMICRF_EUNSUPPORTED;
-    const dim3 g((unsigned)((items + 255) / 256)), t(256);
+    while (a.lanes < 8 && (16 / act_bytes(type)) << a.lanes < D) ++a.lanes;
+    const int rows = ROWS * (256 >> a.lanes);
+    if ((double)B * ((T + rows - 1) / rows) > 2e9) return SEMICRF_EUNSUPPORTED;
+    const dim3 g((unsigned)B * ((T + rows - 1) / rows)), t(256);
     const hipStream_t st = (hipStream_t)stream;
     if (type == ACT_BF16) hipLaunchKernelGGL((k_embed_fwd<__bf16>), g, t, 0, st, a);
     else if (type == ACT_F16) hipLaunchKernelGGL((k_embed_fwd<_Float16>), g, t, 0, st, a);
@@ -301,20 +371,22 @@ int semicrf_embed_bwd(const int32_t *tokens, const int32_t *lengths, const void 
     char *w = (char *)workspace;
     for (int k = 0; k < 2; ++k) a.key[k] = (uint32_t *)(w + p.key[k]), a.pos[k] = (uint32_t *)(w + p.pos[k]);
     a.count = (uint32_t *)(w + p.count);
-    a.start = (uint32_t *)(w + p.start);
+    a.digit = (uint32_t *)(w + p.digit);
+    a.fills = 2 * p.passes;
     a.part = (float *)(w + p.part);
     const hipStream_t st = (hipStream_t)stream;
     for (int pass = 0; pass < p.passes; ++pass) {
-        hipLaunchKernelGGL(k_sort_count, dim3(p.tiles), dim3(256), 0, st, a, 8 * pass);
-        hipLaunchKernelGGL(k_sort_offsets, dim3(1), dim3(1024), 0, st, a);
-        hipLaunchKernelGGL(k_sort_scatter, dim3(p.tiles), dim3(256), 0, st, a, 8 * pass);
+        if (p.large) hipLaunchKernelGGL((k_sort_count<8>), dim3(p.tiles + CLEAR), dim3(256), 0, st, a, 8 * pass);
+        else hipLaunchKernelGGL((k_sort_count<2>), dim3(p.tiles + CLEAR), dim3(256), 0, st, a, 8 * pass);
+        hipLaunchKernelGGL(k_sort_offsets, dim3(RADIX), dim3(64), 0, st, a);
+        if (p.large) hipLaunchKernelGGL((k_sort_scatter<8>), dim3(p.tiles + CLEAR), dim3(256), 0, st, a, 8 * pass);
+        else hipLaunchKernelGGL((k_sort_scatter<2>), dim3(p.tiles + CLEAR), dim3(256), 0, st, a, 8 * pass);
     }
     const uint32_t *key = a.key[p.passes & 1], *pos = a.pos[p.passes & 1];
-    hipLaunchKernelGGL(k_embed_starts, dim3((V + 256) / 256), dim3(256), 0, st, a, key);
     if (type == ACT_BF16) embed_sum<__bf16>(a, key, pos, st);
     else if (type == ACT_F16) embed_sum<_Float16>(a, key, pos, st);
     else embed_sum<float>(a, key, pos, st);
-    hipLaunchKernelGGL(k_embed_join, dim3((unsigned)((int64_t)V * ((D + 255) / 256))), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(k_embed_join, dim3((p.chunks + 3) / 4), dim3(256), 0, st, a, key);
     return launched();
 }
 

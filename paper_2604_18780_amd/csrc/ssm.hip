@@ -198,41 +198,43 @@ struct StepArgs {
     bool linear;
 };
 
-constexpr int STEP_ROWS = 16;  // rows of a head's state that a workgroup owns
-
-// One launch for the whole step: a workgroup owns 16 rows of one head's [P x N] state (16 lanes a row), and convolves what it
-// needs for them: its 16 channels of x and its group's B and C, again in every workgroup of the group (2 N W multiply-adds)
+// One launch for the whole step: a workgroup owns 16 R rows of one head's [P x N] state (16 lanes to a row), and convolves what it
+// needs for them: its channels of x and its group's B and C, again in every workgroup of the group (2 N W multiply-adds)
 // rather than in a launch before this one.  The ring holds the last W tokens at slot (position mod W), so the one slot that
 // is written is the one nobody reads.
-// Bound by the state, read and written once; the loads are on their way before the convolution starts.
-template <class T> __global__ __launch_bounds__(256) void k_ssm_step(StepArgs a)
+// Bound by the state, read and written once; its loads are on their way before the convolution starts.  Sixteen rows to a workgroup
+// spread one stream over the chip; where there are workgroups enough, 64 rows convolve B and C a quarter as often.
+template <class T, int R> __global__ __launch_bounds__(256) void k_ssm_step(StepArgs a)
 {
-    __shared__ float sx[STEP_ROWS], sb[128], sc[128];
-    const int tid = threadIdx.x, tiles = (a.P + STEP_ROWS - 1) / STEP_ROWS;
+    constexpr int ROWS = 16 * R;
+    __shared__ float sx[ROWS], sb[128], sc[128];
+    const int tid = threadIdx.x, tiles = (a.P + ROWS - 1) / ROWS;
     const int tile = blockIdx.x % tiles, h = blockIdx.x / tiles % a.H, b = blockIdx.x / tiles / a.H;
     const int grp = h / (a.H / a.G), channels = a.H * a.P + 2 * a.G * a.N;
-    const int p = tile * STEP_ROWS + tid / 16, q = tid % 16;
-    const size_t cell = (((size_t)b * a.H + h) * a.P + p) * a.N;
-    f4 s[2];
+    const int p0 = tile * ROWS + tid / 16, q = tid % 16;
+    const size_t cell = (((size_t)b * a.H + h) * a.P + p0) * a.N;  // rows p0, p0 + 16, ..
+    f4 s[R][2];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int n = 4 * (q + 16 * k);
-        if (p < a.P && n < a.N) s[k] = *(const f4 *)(a.state + cell + n);
-    }
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int n = 4 * (q + 16 * k);
+            if (p0 + 16 * r < a.P && n < a.N) s[r][k] = *(const f4 *)(a.state + cell + (size_t)16 * r * a.N + n);
+        }
     const int seen = a.seen[b], W = a.W;
     const bool live = seen >= 0;
     const float raw = live ? (float)((const T *)a.dt)[b * a.dt_row + h] + (a.dt_bias ? a.dt_bias[h] : 0.0f) : 0.0f;
     const int slot = live ? seen % W : -1;
-    for (int k = tid; k < STEP_ROWS + 2 * a.N; k += 256) {
+    for (int k = tid; k < ROWS + 2 * a.N; k += 256) {
         int ch;
         float *to;
         bool mine = true;  // whether this workgroup writes the channel's ring
-        if (k < STEP_ROWS) {
-            if (tile * STEP_ROWS + k >= a.P) continue;
-            ch = h * a.P + tile * STEP_ROWS + k;
+        if (k < ROWS) {
+            if (tile * ROWS + k >= a.P) continue;
+            ch = h * a.P + tile * ROWS + k;
             to = sx + k;
         } else {
-            const int n = (k - STEP_ROWS) % a.N, which = (k - STEP_ROWS) / a.N;
+            const int which = k - ROWS >= a.N, n = k - ROWS - which * a.N;
             ch = a.H * a.P + (which * a.G + grp) * a.N + n;
             to = (which ? sc : sb) + n;
             mine = tile == 0 && h % (a.H / a.G) == 0;
@@ -243,7 +245,7 @@ template <class T> __global__ __launch_bounds__(256) void k_ssm_step(StepArgs a)
         float v = a.bias ? a.bias[ch] : 0.0f;
         for (int j = 0; j < W; ++j) {
             // slot j holds the newest position up to `seen` that is j mod W
-            const int back = live ? (slot - j + W) % W : 0;
+            const int back = !live ? 0 : slot >= j ? slot - j : slot - j + W;
             const T held = j == slot ? fresh : ring[j];
             if (live && back <= seen) v += a.weight[ch * W + W - 1 - back] * (float)held;
             if (mine && (ring_out != ring || j == slot)) ring_out[j] = held;
@@ -251,29 +253,46 @@ template <class T> __global__ __launch_bounds__(256) void k_ssm_step(StepArgs a)
         *to = a.linear ? v : v * sigmoid(v);
     }
     __syncthreads();
-    const float delta = softplus(raw), keep = expf(delta * a.rate[h]);
-    const float x = p < a.P ? sx[tid / 16] : 0.0f, u = delta * x;
-    float y = 0.0f;
+    const float delta = softplus(raw), keep = expf(delta * a.rate[h]), skip = a.skip ? a.skip[h] : 0.0f;
+    f4 vb[2], vc[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         const int n = 4 * (q + 16 * k);
-        if (p < a.P && n < a.N) {
-            if (live) {
+        vb[k] = vc[k] = (f4)0.0f;
+        if (n < a.N) vb[k] = *(const f4 *)(sb + n), vc[k] = *(const f4 *)(sc + n);
+    }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[k][e] = s[k][e] * keep + u * sb[n + e];
-                    y += s[k][e] * sc[n + e];
+    for (int r = 0; r < R; ++r) {
+        const int p = p0 + 16 * r;
+        const bool in = p < a.P;
+        const float x = in ? sx[tid / 16 + 16 * r] : 0.0f, u = delta * x;
+        float y = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int n = 4 * (q + 16 * k);
+            if (in && n < a.N) {
+                if (live) {
+                    s[r][k] = s[r][k] * keep + u * vb[k];
+                    const f4 m = s[r][k] * vc[k];
+                    y += m[0] + m[1] + m[2] + m[3];
                 }
+                if (live || a.state_out != a.state) *(f4 *)(a.state_out + cell + (size_t)16 * r * a.N + n) = s[r][k];
             }
-            if (live || a.state_out != a.state) *(f4 *)(a.state_out + cell + n) = s[k];
+        }
+#pragma unroll
+        for (int d = 1; d < 16; d *= 2) y += __shfl_xor(y, d);
+        if (q == 0 && in) {
+            const float o[1] = {live ? y + skip * x : 0.0f};
+            store_n<T, 1>((T *)a.y + ((size_t)b * a.H + h) * a.P + p, o);
         }
     }
-#pragma unroll
-    for (int d = 1; d < 16; d *= 2) y += __shfl_xor(y, d);
-    if (q == 0 && p < a.P) {
-        const float o[1] = {live ? y + (a.skip ? a.skip[h] : 0.0f) * x : 0.0f};
-        store_n<T, 1>((T *)a.y + ((size_t)b * a.H + h) * a.P + p, o);
-    }
+}
+
+template <class T> void launch_step(const StepArgs &a, hipStream_t st)
+{
+    const int64_t whole = (int64_t)a.B * a.H * ((a.P + 63) / 64);
+    if (whole >= 1024) hipLaunchKernelGGL((k_ssm_step<T, 4>), dim3((unsigned)whole), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_ssm_step<T, 1>), dim3((unsigned)(a.B * a.H * ((a.P + 15) / 16))), dim3(256), 0, st, a);
 }
 
 // ---- planning -----------------------------------------------------------------------------------------------------
@@ -479,19 +498,18 @@ int semicrf_ssm_step(const void *u, int64_t u_row, const float *weight, const fl
 {
     if (B < 1 || H < 1 || P < 1 || G < 1 || N < 1 || H % G || W < 1) return SEMICRF_EINVAL;
     const int64_t channels = (int64_t)H * P + 2 * (int64_t)G * N;
-    const int tiles = (P + STEP_ROWS - 1) / STEP_ROWS, type = act_type(flags);
-    if (P % 8 || N % 8 || P > 128 || N > 128 || W > 4 || (double)B * H * tiles > 2e9 || channels > 1e8)
+    const int type = act_type(flags);
+    if (P % 8 || N % 8 || P > 128 || N > 128 || W > 4 || (double)B * H * ((P + 15) / 16) > 2e9 || channels > 1e8)
         return SEMICRF_EUNSUPPORTED;
     if (type < 0 || !u || u_row < channels || !weight || !dt || dt_row < H || !rate || !seen || !ring || !state || !y ||
         !ring_out || !state_out || (((uintptr_t)state | (uintptr_t)state_out) & 15))
         return SEMICRF_EINVAL;
     StepArgs a = {u, dt, ring, u_row, dt_row, weight, bias, rate, skip, dt_bias, state, seen, B, H, P, G, N, W,
                   y, ring_out, state_out, (flags & SEMICRF_CONV_LINEAR) != 0};
-    const dim3 g((unsigned)(B * H * tiles)), t(256);
     const hipStream_t st = (hipStream_t)stream;
-    if (type == ACT_BF16) hipLaunchKernelGGL((k_ssm_step<__bf16>), g, t, 0, st, a);
-    else if (type == ACT_F16) hipLaunchKernelGGL((k_ssm_step<_Float16>), g, t, 0, st, a);
-    else hipLaunchKernelGGL((k_ssm_step<float>), g, t, 0, st, a);
+    if (type == ACT_BF16) launch_step<__bf16>(a, st);
+    else if (type == ACT_F16) launch_step<_Float16>(a, st);
+    else launch_step<float>(a, st);
     return launched();
 }
 
