@@ -41,7 +41,7 @@ struct SsmArgs {
     float *partc, *partb;     // [chunks][B*T][G][N] gradients of C and B by workgroup, where there are several
     float *rint, *dlin, *qint, *xdu;  // [B*H][T] see k_ssm_steps
     float *skipp;             // [B*H][nseg]
-    double *cross;            // [B*H][nseg+1] pairs that cross a segment's boundary
+    double *cross;            // [B*H][nseg+1][P*N/256] pairs that cross a segment's boundary, by wave of k_ssm_chain
     double *headp;            // [B*H*nseg][2] sums for rate and bias
 };
 
@@ -54,7 +54,8 @@ constexpr int GRAD_HEADS = 2;
 constexpr int grad_block(int raw, int dim) { return raw * dim <= 32 ? 64 : 32; }
 
 // one instantiation per storage type, each in a translation unit of its own
-template <class T> int ssm_scan(bool out, bool rev, const SsmArgs &a, hipStream_t st);
+// outputs, or states alone: forwards, or both ways in one launch
+template <class T> int ssm_scan(bool out, bool both, const SsmArgs &a, hipStream_t st);
 extern template int ssm_scan<float>(bool, bool, const SsmArgs &, hipStream_t);
 extern template int ssm_scan<_Float16>(bool, bool, const SsmArgs &, hipStream_t);
 extern template int ssm_scan<__bf16>(bool, bool, const SsmArgs &, hipStream_t);

@@ -3,29 +3,39 @@
 
 namespace semicrf_enc {
 
-// States at the segments' boundaries from what each segment adds: H_{s+1} = kept_s H_s + added_s forwards, and the same
-// backwards for gradients of states.  A thread owns four entries.
-template <bool REV> __global__ __launch_bounds__(256) void k_ssm_chain(SsmArgs a)
+// States at the segments' boundaries from what each segment adds: H_{s+1} = kept_s H_s + added_s forwards, and with `grad` the
+// same backwards for gradients of states, and the pairs of positions that cross each boundary: <G, H> there, by wave.  A
+// thread owns four entries, a workgroup is a wave, so that few heads still reach most of the chip; the loads of sixteen segments
+// are on their way at once.
+template <bool REV> __device__ __forceinline__ void chain_line(const SsmArgs &a, size_t bh, size_t at, bool mine, double *cross, size_t parts)
 {
     const size_t cells = (size_t)a.P * a.N;
-    const unsigned wide = (unsigned)((cells / 4 + 255) / 256);
-    const size_t at = (size_t)(blockIdx.x % wide * 256 + threadIdx.x) * 4, bh = blockIdx.x / wide;
-    if (at >= cells) return;
     float *line = (REV ? a.gs : a.hs) + bh * (a.nseg + 1) * cells + at;
-    const float *first = REV ? a.grad_last : a.state;
+    const float *first = REV ? a.grad_last : a.state, *states = a.hs ? a.hs + bh * (a.nseg + 1) * cells + at : nullptr;
     float *last = REV ? a.gstate : a.state_out;
     const float *kept = a.kept + bh * a.nseg;
-    f4 h = first ? *(const f4 *)(first + bh * cells + at) : (f4)0.0f;
-    *(f4 *)(line + (REV ? (size_t)a.nseg * cells : 0)) = h;
-    constexpr int AHEAD = 8;
+    constexpr int AHEAD = REV ? 8 : 16;
+    f4 h = first && mine ? *(const f4 *)(first + bh * cells + at) : (f4)0.0f;
+    if (mine) *(f4 *)(line + (REV ? (size_t)a.nseg * cells : 0)) = h;
+    double pairs[AHEAD];
+    auto product = [&](f4 g, f4 h) { return (double)g[0] * h[0] + (double)g[1] * h[1] + (double)g[2] * h[2] + (double)g[3] * h[3]; };
+    auto put = [&](int boundary, double s) {
+        for (int d = 1; d < 64; d *= 2) s += __shfl_xor(s, d);
+        if (threadIdx.x == 0) cross[(bh * (a.nseg + 1) + boundary) * parts] = s;
+    };
+    if constexpr (REV) put(a.nseg, mine ? product(h, *(const f4 *)(states + (size_t)a.nseg * cells)) : 0.0);
     for (int s0 = 0; s0 < a.nseg; s0 += AHEAD) {
-        f4 added[AHEAD];
+        f4 added[AHEAD], there[REV ? AHEAD : 1];
         float k[AHEAD];
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            if (s0 + i < a.nseg) {
+            added[i] = (f4)0.0f;
+            if constexpr (REV) there[i] = (f4)0.0f;
+            k[i] = 0.0f, pairs[i] = 0.0;
+            if (s0 + i < a.nseg && mine) {
                 const int s = REV ? a.nseg - 1 - s0 - i : s0 + i;
                 added[i] = *(const f4 *)(line + (size_t)(REV ? s : s + 1) * cells);
+                if constexpr (REV) there[i] = *(const f4 *)(states + (size_t)s * cells);
                 k[i] = kept[s];
             }
         }
@@ -34,27 +44,31 @@ template <bool REV> __global__ __launch_bounds__(256) void k_ssm_chain(SsmArgs a
             if (s0 + i < a.nseg) {
                 const int s = REV ? a.nseg - 1 - s0 - i : s0 + i;
                 h = k[i] * h + added[i];
-                *(f4 *)(line + (size_t)(REV ? s : s + 1) * cells) = h;
+                if (mine) *(f4 *)(line + (size_t)(REV ? s : s + 1) * cells) = h;
+                if constexpr (REV) pairs[i] = product(h, there[i]);
             }
         }
+        if constexpr (REV) {
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2)
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) pairs[i] += __shfl_xor(pairs[i], d);
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                if (s0 + i < a.nseg && threadIdx.x == 0) cross[(bh * (a.nseg + 1) + a.nseg - 1 - s0 - i) * parts] = pairs[i];
+        }
     }
-    if (last) *(f4 *)(last + bh * cells + at) = h;
+    if (last && mine) *(f4 *)(last + bh * cells + at) = h;
 }
 
-// Pairs of positions that cross a segment's boundary: <G, H> there, G the gradient of the state H.  One wave per boundary.
-__global__ __launch_bounds__(256) void k_ssm_cross(SsmArgs a)
+__global__ __launch_bounds__(64) void k_ssm_chain(SsmArgs a, bool grad)
 {
-    const int lane = threadIdx.x & 63;
-    const size_t at = (size_t)blockIdx.x * 4 + threadIdx.x / 64, cells = (size_t)a.P * a.N;
-    if (at >= (size_t)a.B * a.H * (a.nseg + 1)) return;
-    const f4 *hs = (const f4 *)(a.hs + at * cells), *gs = (const f4 *)(a.gs + at * cells);
-    double s = 0.0;
-    for (size_t k = lane; k < cells / 4; k += 64) {
-        const f4 p = hs[k], q = gs[k];
-        s += (double)p[0] * q[0] + (double)p[1] * q[1] + (double)p[2] * q[2] + (double)p[3] * q[3];
-    }
-    for (int d = 1; d < 64; d *= 2) s += __shfl_xor(s, d);
-    if (lane == 0) a.cross[at] = s;
+    const size_t cells = (size_t)a.P * a.N;
+    const unsigned parts = (unsigned)((cells / 4 + 63) / 64);
+    const size_t at = (size_t)(blockIdx.x % parts * 64 + threadIdx.x) * 4, bh = blockIdx.x / parts;
+    const bool mine = at < cells;
+    chain_line<false>(a, bh, at, mine, nullptr, 0);
+    if (grad) chain_line<true>(a, bh, at, mine, a.cross + blockIdx.x % parts, parts);
 }
 
 // Gradients of the steps.  l_t multiplies everything that passes step t: pairs (i, j) with j < t <= i, of four kinds by block:
@@ -62,7 +76,7 @@ __global__ __launch_bounds__(256) void k_ssm_cross(SsmArgs a)
 //   rint[i]  from before the block to i in it; those with i >= t count,
 //   qint[j]  from j in the block to behind it; those with j < t count,
 //   across   from before the block to behind it.
-// The pairs that cross a boundary are known at a segment's ends (k_ssm_cross).  From the later one backwards, taking off those that
+// The pairs that cross a boundary are known at a segment's ends (k_ssm_chain).  From the later one backwards, taking off those that
 // begin in a block leaves its `across`, and adding those that end in it gives what crosses its start.  Rounding adds up along that
 // walk, and all positions of a block share it: what the walk is off by at the segment's start is taken back in equal parts.
 // Where a block keeps less than 2^-30, nothing is left of the difference but rounding: `across` is 0, and the walk begins
@@ -71,27 +85,43 @@ constexpr int MOST_BLOCKS = 16;  // of a segment of 512
 
 template <class T> __global__ __launch_bounds__(64) void k_ssm_steps(SsmArgs a)
 {
-    __shared__ double over[MOST_BLOCKS];
+    __shared__ double over[MOST_BLOCKS], qs[MOST_BLOCKS], rs[MOST_BLOCKS];
+    __shared__ float ks[MOST_BLOCKS];
     const int lane = threadIdx.x, Q = a.block, r = lane & (Q - 1);
     const int seg = blockIdx.x % a.nseg, bh = blockIdx.x / a.nseg, h = bh % a.H, b = bh / a.H;
     const int L = length_of(a.lengths, b, a.T);
     const int t0 = seg * a.seg, t1 = t0 + a.seg < a.T ? t0 + a.seg : a.T;
-    const int used = (t1 < L ? t1 : L) - t0, nblk = used > 0 ? (used + Q - 1) / Q : 0;
+    const int used = (t1 < L ? t1 : L) - t0, nblk = used > 0 ? (used + Q - 1) / Q : 0, end = t0 + (used > 0 ? used : 0);
     T *gdt = (T *)a.gdt + (int64_t)b * a.T * a.gdt_row + h;
     const T *dts = (const T *)a.dt + (int64_t)b * a.T * a.dt_row + h;
     const float rate = a.rate[h], bias = a.dt_bias ? a.dt_bias[h] : 0.0f;
-    const double *cross = a.cross + (size_t)bh * (a.nseg + 1) + seg;
+    // sums of each block, 64 positions (two blocks of 32, or one of 64) at a time
+    for (int i = t0; i < end; i += 64) {
+        const int t = i + lane;
+        const bool in = t < end;
+        const size_t at = (size_t)bh * a.T + t;
+        double q = in ? (double)a.qint[at] : 0.0, ri = in ? (double)a.rint[at] : 0.0;
+        float kept = in ? softplus((float)dts[t * a.dt_row] + bias) : 0.0f;
+        for (int d = 1; d < Q; d *= 2) q += __shfl_xor(q, d), ri += __shfl_xor(ri, d), kept += __shfl_xor(kept, d);
+        const int n = (i - t0 + lane) / Q;
+        if (r == 0 && n < nblk) qs[n] = q, rs[n] = ri, ks[n] = kept;
+    }
+    double cross[2] = {0.0, 0.0};
+    {
+        const int parts = (a.P * a.N / 4 + 63) / 64;
+        const double *from = a.cross + ((size_t)bh * (a.nseg + 1) + seg) * parts;
+        for (int e = 0; e < 2; ++e) {
+            if (lane < parts) cross[e] = from[(size_t)e * parts + lane];
+            for (int d = 1; d < 64; d *= 2) cross[e] += __shfl_xor(cross[e], d);
+        }
+    }
+    __syncthreads();
     {
         double across = cross[1];
         int first = nblk;  // the walk's blocks: up to here
         for (int n = nblk - 1; n >= 0; --n) {
-            const int t = t0 + Q * n + lane;
-            const bool in = lane < Q && t < L && t < t1;
-            const size_t at = (size_t)bh * a.T + t;
-            float kept = in ? softplus((float)dts[t * a.dt_row] + bias) : 0.0f;
-            double ri = in ? (double)a.rint[at] : 0.0, qi = in ? (double)a.qint[at] : 0.0;
-            for (int d = 1; d < 64; d *= 2) kept += __shfl_xor(kept, d), ri += __shfl_xor(ri, d), qi += __shfl_xor(qi, d);
-            const bool gone = kept * rate * 1.44269504f < -30.0f;
+            const double qi = qs[n], ri = rs[n];
+            const bool gone = ks[n] * rate * 1.44269504f < -30.0f;
             const double off = gone ? across - qi : n == 0 ? across - qi + ri - cross[0] : 0.0;
             across -= qi;
             if (lane == 0) over[n] = across;
@@ -100,8 +130,8 @@ template <class T> __global__ __launch_bounds__(64) void k_ssm_steps(SsmArgs a)
                 __syncthreads();
                 const int m = first - n;
                 if (lane < m) over[n + lane] -= off * (double)(m - lane) / m;
-                if (gone && lane == 0) over[n] = 0.0;
                 __syncthreads();
+                if (gone && lane == 0) over[n] = 0.0;
                 first = n;
                 across = 0.0;
             }
@@ -110,16 +140,15 @@ template <class T> __global__ __launch_bounds__(64) void k_ssm_steps(SsmArgs a)
     }
     __syncthreads();
     double grate = 0.0, gbias = 0.0;
-    for (int n = 0; n < nblk; ++n) {
-        const int t = t0 + Q * n + r;
-        const bool in = t < L && t < t1;
+    for (int i = t0; i < end; i += 64) {
+        const int t = i + lane;
+        const bool in = t < end;
         const size_t at = (size_t)bh * a.T + t;
         float tail = 0.0f, qi = 0.0f, own = 0.0f, dx = 0.0f, raw = 0.0f;
         if (in) {
             tail = a.rint[at], own = a.dlin[at], qi = a.qint[at], dx = a.xdu[at];
             raw = (float)dts[t * a.dt_row] + bias;
         }
-        // over the block's lanes (the other half of the wave repeats them where a block is 32)
         float head = __shfl_up(qi, 1);
         if (r == 0) head = 0.0f;
         for (int d = 1; d < Q; d *= 2) {
@@ -127,8 +156,8 @@ template <class T> __global__ __launch_bounds__(64) void k_ssm_steps(SsmArgs a)
             if (r + d < Q) tail += o;
             if (r >= d) head += p;
         }
-        if (in && lane < Q) {
-            const float dl = own + tail + head + (float)over[n], g = (dx + rate * dl) * sigmoid(raw);
+        if (in) {
+            const float dl = own + tail + head + (float)over[(t - t0) / Q], g = (dx + rate * dl) * sigmoid(raw);
             const float one[1] = {g};
             store_n<T, 1>(gdt + t * a.gdt_row, one);
             grate += (double)dl * softplus(raw);
@@ -349,7 +378,7 @@ int make_ssm_plan(int B, int T, int H, int P, int G, int N, bool grad, SsmPlan *
         p->qint = take(rows * H * 4);
         p->xdu = take(rows * H * 4);
         p->skipp = take(bh * p->nseg * 4);
-        p->cross = take(bh * (p->nseg + 1) * 8);
+        p->cross = take(bh * (p->nseg + 1) * ((cells / 4 + 63) / 64) * 8);
         p->headp = take(bh * p->nseg * 16);
     }
     p->total = at;
@@ -363,18 +392,16 @@ int grad(int type, const SsmArgs &a, hipStream_t st)
     return ssm_grad<float>(a, st);
 }
 
-int scan(int type, bool out, bool rev, const SsmArgs &a, hipStream_t st)
+int scan(int type, bool out, bool both, const SsmArgs &a, hipStream_t st)
 {
-    if (type == ACT_BF16) return ssm_scan<__bf16>(out, rev, a, st);
-    if (type == ACT_F16) return ssm_scan<_Float16>(out, rev, a, st);
-    return ssm_scan<float>(out, rev, a, st);
+    if (type == ACT_BF16) return ssm_scan<__bf16>(out, both, a, st);
+    if (type == ACT_F16) return ssm_scan<_Float16>(out, both, a, st);
+    return ssm_scan<float>(out, both, a, st);
 }
 
-int chain(bool rev, const SsmArgs &a, hipStream_t st)
+int chain(bool grad, const SsmArgs &a, hipStream_t st)
 {
-    const dim3 g((unsigned)((a.P * a.N / 4 + 255) / 256 * a.B * a.H)), t(256);
-    if (rev) hipLaunchKernelGGL((k_ssm_chain<true>), g, t, 0, st, a);
-    else hipLaunchKernelGGL((k_ssm_chain<false>), g, t, 0, st, a);
+    hipLaunchKernelGGL(k_ssm_chain, dim3((unsigned)((a.P * a.N / 4 + 63) / 64 * a.B * a.H)), dim3(64), 0, st, a, grad);
     return launched();
 }
 
@@ -470,12 +497,9 @@ int semicrf_ssm_bwd(const void *x, int64_t x_row, const void *b, int64_t b_row, 
     const int most = P > N ? P : N;
     a.heads = p.heads; a.chunks = p.chunks;
     a.block = grad_block(type == ACT_F32 ? 3 : type == ACT_F16 ? 2 : 1, most <= 32 ? 32 : most <= 64 ? 64 : 128);
-    if (int rc = scan(type, false, false, a, st)) return rc;
     if (int rc = scan(type, false, true, a, st)) return rc;
-    if (int rc = chain(false, a, st)) return rc;
     if (int rc = chain(true, a, st)) return rc;
     if (int rc = grad(type, a, st)) return rc;
-    hipLaunchKernelGGL(k_ssm_cross, dim3((unsigned)(((int64_t)B * H * (p.nseg + 1) + 3) / 4)), dim3(256), 0, st, a);
     const dim3 steps(B * H * p.nseg), heads((unsigned)(((int64_t)B * T * G * (N / 4) + 255) / 256), 2);
     if (type == ACT_BF16) {
         hipLaunchKernelGGL((k_ssm_steps<__bf16>), steps, dim3(64), 0, st, a);

@@ -16,22 +16,31 @@
 
 namespace semicrf_enc {
 
-template <class T, int Q, int DK, int PV, bool OUT, bool REV> __global__ __launch_bounds__(PV * 4, 2) void k_ssm_scan(SsmArgs a)
+// LDS of a workgroup.
+template <class T, int Q, int DK, int PV, bool OUT> struct ScanShared {
+    static constexpr int NW = PV / 16, AHEAD = NW < 4 ? NW : 4;  // blocks whose steps are made together, one by each wave
+    typedef Tile<T, Q, DK, PV * 4, false> TK;
+    typedef Tile<T, Q, PV, PV * 4, false> TV;
+    // one array, so that operands' places differ by constants
+    __bf16 pool[(OUT ? 2 : 1) * TK::ELEMS + TV::ELEMS + (OUT ? Scores<Q, Parts<T>::made>::ELEMS : 0)];
+    Steps<Q> ss[AHEAD];
+};
+
+template <class T, int Q, int DK, int PV, bool OUT, bool REV>
+__device__ __forceinline__ void scan_segment(const SsmArgs &a, unsigned block, ScanShared<T, Q, DK, PV, OUT> &sh)
 {
     constexpr int NT = PV * 4, NW = PV / 16, KT = DK / 16, KS = DK / 32, IT = Q / 16, QS = Q / 32;
-    constexpr int AHEAD = NW < 4 ? NW : 4;  // blocks whose steps are made together, one by each wave
+    constexpr int AHEAD = ScanShared<T, Q, DK, PV, OUT>::AHEAD;
     constexpr int RAW = Parts<T>::raw, MADE = Parts<T>::made, HELD = 3;
     typedef Tile<T, Q, DK, NT, REV> TK;
     typedef Tile<T, Q, PV, NT, REV> TV;
     typedef Scores<Q, MADE> SC;
-    // one array, so that operands' places differ by constants
-    __shared__ __attribute__((aligned(16))) __bf16 pool[(OUT ? 2 : 1) * TK::ELEMS + TV::ELEMS + (OUT ? SC::ELEMS : 0)];
-    __bf16 *const sk = pool, *const sv = sk + TK::ELEMS, *const sq = sv + TV::ELEMS, *const sm = sq + (OUT ? TK::ELEMS : 0);
-    __shared__ __attribute__((aligned(16))) Steps<Q> ss[AHEAD];
+    __bf16 *const sk = sh.pool, *const sv = sk + TK::ELEMS, *const sq = sv + TV::ELEMS, *const sm = sq + (OUT ? TK::ELEMS : 0);
+    Steps<Q> *const ss = sh.ss;
 
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, i16 = lane & 15;
     // heads of one segment follow each other on one XCD (workgroups go round the eight in turn): they share B and C
-    const int unit = (blockIdx.x % 8) + 8 * (blockIdx.x / 8 / a.H), h = blockIdx.x / 8 % a.H;
+    const int unit = (block % 8) + 8 * (block / 8 / a.H), h = block / 8 % a.H;
     if (unit >= a.B * a.nseg) return;
     const int b = unit / a.nseg, seg = unit % a.nseg, grp = h / (a.H / a.G), bh = b * a.H + h;
     const int L = __builtin_amdgcn_readfirstlane(length_of(a.lengths, b, a.T));
@@ -195,30 +204,42 @@ template <class T, int Q, int DK, int PV, bool OUT, bool REV> __global__ __launc
     }
 }
 
-template <class T, int Q, int DK, int PV> int launch_scan(bool out, bool rev, const SsmArgs &a, hipStream_t st)
+template <class T, int Q, int DK, int PV> __global__ __launch_bounds__(PV * 4, 2) void k_ssm_scan(SsmArgs a)
+{
+    __shared__ __attribute__((aligned(16))) ScanShared<T, Q, DK, PV, true> sh;
+    scan_segment<T, Q, DK, PV, true, false>(a, blockIdx.x, sh);
+}
+// States alone, forwards or (the second half of a launch of twice as many workgroups) backwards.
+template <class T, int Q, int DK, int PV> __global__ __launch_bounds__(PV * 4, 2) void k_ssm_states(SsmArgs a, unsigned half)
+{
+    __shared__ __attribute__((aligned(16))) ScanShared<T, Q, DK, PV, false> sh;
+    if (blockIdx.x < half) scan_segment<T, Q, DK, PV, false, false>(a, blockIdx.x, sh);
+    else scan_segment<T, Q, DK, PV, false, true>(a, blockIdx.x - half, sh);
+}
+
+template <class T, int Q, int DK, int PV> int launch_scan(bool out, bool both, const SsmArgs &a, hipStream_t st)
 {
     const long grid = ((long)a.B * a.nseg + 7) / 8 * 8 * a.H;
-    if (grid > 0x7fffffffL) return SEMICRF_EUNSUPPORTED;
-    const dim3 g((unsigned)grid), t(PV * 4);
-    if (out) hipLaunchKernelGGL((k_ssm_scan<T, Q, DK, PV, true, false>), g, t, 0, st, a);
-    else if (!rev) hipLaunchKernelGGL((k_ssm_scan<T, Q, DK, PV, false, false>), g, t, 0, st, a);
-    else hipLaunchKernelGGL((k_ssm_scan<T, Q, DK, PV, false, true>), g, t, 0, st, a);
+    if (grid > 0x3fffffffL) return SEMICRF_EUNSUPPORTED;
+    const dim3 t(PV * 4);
+    if (out) hipLaunchKernelGGL((k_ssm_scan<T, Q, DK, PV>), dim3((unsigned)grid), t, 0, st, a);
+    else hipLaunchKernelGGL((k_ssm_states<T, Q, DK, PV>), dim3((unsigned)(both ? 2 * grid : grid)), t, 0, st, a, (unsigned)grid);
     return launched();
 }
-template <class T, int DK> int launch_scan_p(bool out, bool rev, const SsmArgs &a, hipStream_t st)
+template <class T, int DK> int launch_scan_p(bool out, bool both, const SsmArgs &a, hipStream_t st)
 {
     // blocks of 64 as long as the staged parts leave room for two workgroups on a compute unit
     constexpr int R = Parts<T>::raw;
-    if (a.P <= 16) return launch_scan<T, R * (2 * DK + 16) <= 448 ? 64 : 32, DK, 16>(out, rev, a, st);
-    if (a.P <= 32) return launch_scan<T, R * (2 * DK + 32) <= 448 ? 64 : 32, DK, 32>(out, rev, a, st);
-    if (a.P <= 64) return launch_scan<T, R * (2 * DK + 64) <= 448 ? 64 : 32, DK, 64>(out, rev, a, st);
-    return launch_scan<T, R * (2 * DK + 128) <= 448 ? 64 : 32, DK, 128>(out, rev, a, st);
+    if (a.P <= 16) return launch_scan<T, R * (2 * DK + 16) <= 448 ? 64 : 32, DK, 16>(out, both, a, st);
+    if (a.P <= 32) return launch_scan<T, R * (2 * DK + 32) <= 448 ? 64 : 32, DK, 32>(out, both, a, st);
+    if (a.P <= 64) return launch_scan<T, R * (2 * DK + 64) <= 448 ? 64 : 32, DK, 64>(out, both, a, st);
+    return launch_scan<T, R * (2 * DK + 128) <= 448 ? 64 : 32, DK, 128>(out, both, a, st);
 }
-template <class T> int ssm_scan(bool out, bool rev, const SsmArgs &a, hipStream_t st)
+template <class T> int ssm_scan(bool out, bool both, const SsmArgs &a, hipStream_t st)
 {
-    if (a.N <= 32) return launch_scan_p<T, 32>(out, rev, a, st);
-    if (a.N <= 64) return launch_scan_p<T, 64>(out, rev, a, st);
-    return launch_scan_p<T, 128>(out, rev, a, st);
+    if (a.N <= 32) return launch_scan_p<T, 32>(out, both, a, st);
+    if (a.N <= 64) return launch_scan_p<T, 64>(out, both, a, st);
+    return launch_scan_p<T, 128>(out, both, a, st);
 }
 
 }  // namespace semicrf_enc
