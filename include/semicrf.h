@@ -418,9 +418,10 @@ int semicrf_seq_report(const void *workspace, size_t workspace_bytes, int B, int
  * of an input are never read, those of an output are written as 0.  A `_row` argument is the distance, in elements, of one
  * token's row from the next; sequence b begins B-major at row b*T.  So x, b and c may be columns of one array (the
  * convolution's output), and gradients may be written side by side into one.  Rows that are read or written 16 bytes
- * at a time (all but dt and grad_dt) begin on 16-byte boundaries (SEMICRF_EINVAL otherwise).  Results do not depend on
- * timing: there are no floating-point atomics.  A value that is not finite in a valid row may spread over that sequence's
- * results (and over the sums over sequences), earlier positions of the same 32 included; other sequences are not touched.
+ * at a time (all but dt and grad_dt) begin on 16-byte boundaries, and a row is at most 2^22 elements long, 2^19 for the
+ * convolution (SEMICRF_EINVAL otherwise).  Results do not depend on timing: there are no floating-point atomics.  A value that
+ * is not finite in a valid row may spread over that sequence's results (and over the sums over sequences), up to 63 earlier
+ * positions and the rows behind its end included; other sequences are not touched.
  */
 
 /* flags bit 11 (semicrf_conv_fwd, semicrf_conv_bwd, semicrf_ssm_step): no SiLU after the convolution. */

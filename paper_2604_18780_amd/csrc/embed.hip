@@ -361,6 +361,7 @@ int semicrf_embed_bwd(const int32_t *tokens, const int32_t *lengths, const void 
     EmbedPlan p = {};
     if (int rc = embed_plan(B, T, V, D, &p)) return rc;
     const int type = act_type(flags);
+    if ((double)p.chunks * (D / 256 + 1) > 2e9) return SEMICRF_EUNSUPPORTED;
     if (type < 0 || !tokens || !rows_ok(grad_out, D, D, type) || !grad_table || ((uintptr_t)grad_table & 15))
         return SEMICRF_EINVAL;
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < p.total) return SEMICRF_EWORKSPACE;

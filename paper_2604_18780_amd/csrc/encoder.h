@@ -19,10 +19,6 @@ typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 template <class T> constexpr int PER16 = 16 / (int)sizeof(T);
 
 // n consecutive elements from / to memory that is aligned to their size, as float.  Narrowing rounds to nearest even.
-template <class T, int n> struct Pack {
-    T v[n];
-};
-
 template <class T, int n> __device__ __forceinline__ void load_n(const T *p, float (&o)[n])
 {
     typedef T V __attribute__((ext_vector_type(n)));

@@ -53,8 +53,8 @@ struct SsmArgs {
 constexpr int GRAD_HEADS = 2;
 constexpr int grad_block(int raw, int dim) { return raw * dim <= 32 ? 64 : 32; }
 
-// one instantiation per storage type, each in a translation unit of its own
-// outputs, or states alone: forwards, or both ways in one launch
+// One instantiation per storage type, each in a translation unit of its own: outputs, or states alone (forwards, or both ways in
+// one launch); and the gradient kernels.
 template <class T> int ssm_scan(bool out, bool both, const SsmArgs &a, hipStream_t st);
 extern template int ssm_scan<float>(bool, bool, const SsmArgs &, hipStream_t);
 extern template int ssm_scan<_Float16>(bool, bool, const SsmArgs &, hipStream_t);

@@ -1,4 +1,4 @@
-// Selective state space scan: the small kernels around the sweeps, the single-token form, and the entry points.
+// Selective state space scan: the small kernels around the scans, the single-token form, and the entry points.
 #include "ssm.h"
 
 namespace semicrf_enc {
@@ -409,7 +409,7 @@ int ssm_inputs(SsmArgs &a, int type, const void *x, int64_t x_row, const void *b
                int64_t c_row, const void *dt, int64_t dt_row, const float *rate, const float *skip,
                const float *dt_bias, const int32_t *lengths, const float *state, int B, int T, int H, int P, int G, int N)
 {
-    if (type < 0 || !dt || !rate || dt_row < H || ((uintptr_t)state & 15)) return SEMICRF_EINVAL;
+    if (type < 0 || !dt || !rate || dt_row < H || dt_row > (1 << 22) || ((uintptr_t)state & 15)) return SEMICRF_EINVAL;
     if (!rows_ok(x, x_row, (int64_t)H * P, type) || !rows_ok(b, b_row, (int64_t)G * N, type) ||
         !rows_ok(c, c_row, (int64_t)G * N, type))
         return SEMICRF_EINVAL;

@@ -183,7 +183,7 @@ __device__ __forceinline__ void scan_segment(const SsmArgs &a, unsigned block, S
     float *to;
     if constexpr (!OUT) {
         to = REV ? a.gs + ((size_t)bh * (a.nseg + 1) + seg) * cells : a.hs + ((size_t)bh * (a.nseg + 1) + seg + 1) * cells;
-        if (tid == 0) a.kept[(size_t)bh * a.nseg + seg] = pow2(gone);
+        if (!REV && tid == 0) a.kept[(size_t)bh * a.nseg + seg] = pow2(gone);
     } else {
         to = !a.hs && a.state_out ? a.state_out + bh * cells : nullptr;
     }
