@@ -7,7 +7,7 @@
 // for each token: a chunk writes the tokens that lie in it whole, and leaves a partial row where one enters from the chunk
 // before or goes on in the next; those are joined in chunk order.  Zeros for tokens that do not occur are written while the
 // positions are sorted, which keeps few workgroups busy.  Bound by g read once and the table written once; for few tokens by the
-// launches: three a pass and two.
+// launches: the sort's one, or two to three a pass, and two.
 #include "encoder.h"
 
 namespace semicrf_enc {
@@ -77,7 +77,12 @@ __device__ __forceinline__ bool clear_share(const EmbedArgs &a, int launch)
     return true;
 }
 
-// How often each digit occurs in each tile of 256 * ROUNDS positions: count[digit][tile].
+// Where the launch that puts positions in their places adds up the tiles' counts by itself: count[tile][digit] then, count[digit][tile]
+// where k_sort_offsets does.  Up to 64 tiles that saves a launch a pass: 16384 positions of 250 tokens, 256 columns, take 18 us
+// instead of 21, 32000 positions (63 tiles) as long with as without.
+constexpr int FEW_TILES = 64;
+
+// How often each digit occurs in each tile of 256 * ROUNDS positions.
 template <int ROUNDS> __global__ __launch_bounds__(256) void k_sort_count(EmbedArgs a, int shift)
 {
     __shared__ uint32_t c[RADIX];
@@ -93,7 +98,7 @@ template <int ROUNDS> __global__ __launch_bounds__(256) void k_sort_count(EmbedA
     for (int k = 0; k < ROUNDS; ++k)
         if (first + 256 * k < a.n) atomicAdd(&c[(key[k] >> shift) % RADIX], 1u);
     __syncthreads();
-    a.count[threadIdx.x * a.tiles + blockIdx.x] = c[threadIdx.x];
+    a.count[a.tiles <= FEW_TILES ? blockIdx.x * RADIX + threadIdx.x : threadIdx.x * a.tiles + blockIdx.x] = c[threadIdx.x];
 }
 
 // Prefix sum of a wave's values, exclusive; `all` is their sum.
@@ -122,6 +127,18 @@ __global__ __launch_bounds__(64) void k_sort_offsets(EmbedArgs a)
     if (threadIdx.x == 0) a.digit[blockIdx.x] = base;
 }
 
+// Lanes of the wave that hold the same digit as this one, of those that are `in`.
+__device__ __forceinline__ uint64_t same_digit(uint32_t d, bool in)
+{
+    uint64_t same = __ballot(in);
+#pragma unroll
+    for (int bit = 0; bit < 8; ++bit) {
+        const uint64_t set = __ballot((d >> bit) & 1);
+        same &= (d >> bit) & 1 ? set : ~set;
+    }
+    return same;
+}
+
 // Puts a tile's positions in their places.  A wave takes 64 positions at a time, in order; a position's place among equal digits
 // is what earlier tiles, waves, rounds and lower lanes hold, so equal keys keep their order.
 template <int ROUNDS> __global__ __launch_bounds__(256) void k_sort_scatter(EmbedArgs a, int shift)
@@ -130,8 +147,17 @@ template <int ROUNDS> __global__ __launch_bounds__(256) void k_sort_scatter(Embe
     if (clear_share(a, shift / 4 + 1)) return;
     const int lane = threadIdx.x % 64, w = threadIdx.x / 64, pass = shift / 8;
     for (int k = 0; k < 4; ++k) c[k][threadIdx.x] = 0;
-    const uint32_t earlier = a.count[threadIdx.x * a.tiles + blockIdx.x], here = a.digit[threadIdx.x];
-    uint32_t all;
+    uint32_t all, earlier = 0, here = 0;  // of the digit `threadIdx.x`: in earlier tiles, in all
+    if (a.tiles <= FEW_TILES) {
+#pragma unroll 8
+        for (int k = 0; k < a.tiles; ++k) {
+            const uint32_t n = a.count[k * RADIX + threadIdx.x];
+            here += n;
+            earlier += k < (int)blockIdx.x ? n : 0;
+        }
+    } else {
+        earlier = a.count[threadIdx.x * a.tiles + blockIdx.x], here = a.digit[threadIdx.x];
+    }
     uint32_t base = before_lane(here, all);
     if (lane == 63) wave[w] = all;
     const int first = blockIdx.x * 256 * ROUNDS + w * 64 * ROUNDS + lane;
@@ -149,12 +175,7 @@ template <int ROUNDS> __global__ __launch_bounds__(256) void k_sort_scatter(Embe
     for (int k = 0; k < ROUNDS; ++k) {
         const bool in = first + 64 * k < a.n;
         const uint32_t d = (key[k] >> shift) % RADIX;
-        uint64_t same = __ballot(in);
-#pragma unroll
-        for (int bit = 0; bit < 8; ++bit) {
-            const uint64_t set = __ballot((d >> bit) & 1);
-            same &= (d >> bit) & 1 ? set : ~set;
-        }
+        const uint64_t same = same_digit(d, in);
         const uint32_t below = __popcll(same & ((1ull << lane) - 1));
         uint32_t before = 0;
         if (in) before = c[w][d];
@@ -177,6 +198,69 @@ template <int ROUNDS> __global__ __launch_bounds__(256) void k_sort_scatter(Embe
             a.key[(pass + 1) & 1][to] = key[k];
             a.pos[(pass + 1) & 1][to] = pos[k];
         }
+}
+
+// The whole sort in one launch, for as many positions as a workgroup holds: a position and its token are one word, positions below,
+// R of them to a thread, and change places through LDS.  The other workgroups clear the gradient meanwhile.
+constexpr int WIDE = 1024, MOST_AT_ONCE = 4 * WIDE;
+template <int R> __global__ __launch_bounds__(WIDE) void k_sort_whole(EmbedArgs a, int bits, int passes)
+{
+    __shared__ uint32_t words[WIDE * R], c[WIDE / 64][RADIX], wave[RADIX / 64];
+    const int tid = threadIdx.x, lane = tid % 64, w = tid / 64, first = w * 64 * R + lane;
+    if (blockIdx.x > 0) {
+        const int64_t all = (int64_t)a.V * a.D / 4;
+        for (int64_t k = (int64_t)(blockIdx.x - 1) * WIDE + tid; k < all; k += (int64_t)(gridDim.x - 1) * WIDE) *(f4 *)(a.grad + 4 * k) = (f4)0.0f;
+        return;
+    }
+    uint32_t word[R], rank[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        const int i = first + 64 * k;
+        word[k] = i < a.n ? key_of(a, i) << bits | (uint32_t)i : ~0u;  // places without a position stay the last
+    }
+    for (int shift = bits; passes > 0; --passes, shift += 8) {
+        for (int k = tid; k < (WIDE / 64) * RADIX; k += WIDE) c[k / RADIX][k % RADIX] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const uint32_t d = (word[k] >> shift) % RADIX;
+            const uint64_t same = same_digit(d, true);
+            const uint32_t below = __popcll(same & ((1ull << lane) - 1)), before = c[w][d];
+            rank[k] = before + below;
+            __builtin_amdgcn_wave_barrier();
+            if (below == 0) c[w][d] = before + (uint32_t)__popcll(same);
+            __builtin_amdgcn_wave_barrier();
+        }
+        __syncthreads();
+        uint32_t held[WIDE / 64], base = 0;
+        if (tid < RADIX) {
+            uint32_t sum = 0, all;
+#pragma unroll
+            for (int k = 0; k < WIDE / 64; ++k) {
+                held[k] = sum;
+                sum += c[k][tid];
+            }
+            base = before_lane(sum, all);
+            if (lane == 0) wave[w] = all;
+        }
+        __syncthreads();
+        if (tid < RADIX) {
+            for (int k = 0; k < w; ++k) base += wave[k];
+#pragma unroll
+            for (int k = 0; k < WIDE / 64; ++k) c[k][tid] = base + held[k];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < R; ++k) words[c[w][(word[k] >> shift) % RADIX] + rank[k]] = word[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < R; ++k) word[k] = words[first + 64 * k];
+    }
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        const int i = first + 64 * k;
+        if (i < a.n) a.key[0][i] = word[k] >> bits, a.pos[0][i] = word[k] & ((1u << bits) - 1);
+    }
 }
 
 // One wave adds up one chunk of the sorted positions over 64 lanes of columns.  Keys and places are a lane's each, read once and
@@ -281,7 +365,7 @@ __global__ __launch_bounds__(256) void k_embed_join(EmbedArgs a, const uint32_t 
 }
 
 struct EmbedPlan {
-    int n, tiles, chunk, chunks, passes;
+    int n, tiles, chunk, chunks, passes, bits;  // bits: of a position, where one workgroup sorts all (0: it does not)
     bool large;
     size_t key[2], pos[2], count, digit, part, total;
 };
@@ -299,6 +383,13 @@ int embed_plan(int B, int T, int V, int D, EmbedPlan *p)
     p->chunks = (p->n + p->chunk - 1) / p->chunk;
     p->passes = 0;
     for (int64_t left = V; left > 0; left >>= 8) ++p->passes;
+    // Up to 4096 positions are sorted in one launch by one workgroup, if a position and its token go into 32 bits: 1000 positions of
+    // 300 tokens, 512 columns, take 15 us instead of 22, 4000 take 19 instead of 22.  16384 would take 36 instead of 18: one
+    // workgroup's ranks take 16 us a pass.
+    int bits = 0;
+    while (p->n > 1 << bits) ++bits;
+    if (bits == 0) bits = 1;
+    p->bits = p->n <= MOST_AT_ONCE && (int64_t)V << bits < (int64_t)1 << 32 ? bits : 0;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t o = at;
@@ -376,14 +467,21 @@ int semicrf_embed_bwd(const int32_t *tokens, const int32_t *lengths, const void 
     a.fills = 2 * p.passes;
     a.part = (float *)(w + p.part);
     const hipStream_t st = (hipStream_t)stream;
-    for (int pass = 0; pass < p.passes; ++pass) {
-        if (p.large) hipLaunchKernelGGL((k_sort_count<8>), dim3(p.tiles + CLEAR), dim3(256), 0, st, a, 8 * pass);
-        else hipLaunchKernelGGL((k_sort_count<2>), dim3(p.tiles + CLEAR), dim3(256), 0, st, a, 8 * pass);
-        hipLaunchKernelGGL(k_sort_offsets, dim3(RADIX), dim3(64), 0, st, a);
-        if (p.large) hipLaunchKernelGGL((k_sort_scatter<8>), dim3(p.tiles + CLEAR), dim3(256), 0, st, a, 8 * pass);
-        else hipLaunchKernelGGL((k_sort_scatter<2>), dim3(p.tiles + CLEAR), dim3(256), 0, st, a, 8 * pass);
+    if (p.bits) {
+        const dim3 g(256), t(WIDE);
+        if (p.n <= WIDE) hipLaunchKernelGGL((k_sort_whole<1>), g, t, 0, st, a, p.bits, p.passes);
+        else hipLaunchKernelGGL((k_sort_whole<4>), g, t, 0, st, a, p.bits, p.passes);
+    } else {
+        for (int pass = 0; pass < p.passes; ++pass) {
+            if (p.large) hipLaunchKernelGGL((k_sort_count<8>), dim3(p.tiles + CLEAR), dim3(256), 0, st, a, 8 * pass);
+            else hipLaunchKernelGGL((k_sort_count<2>), dim3(p.tiles + CLEAR), dim3(256), 0, st, a, 8 * pass);
+            if (p.tiles > FEW_TILES) hipLaunchKernelGGL(k_sort_offsets, dim3(RADIX), dim3(64), 0, st, a);
+            if (p.large) hipLaunchKernelGGL((k_sort_scatter<8>), dim3(p.tiles + CLEAR), dim3(256), 0, st, a, 8 * pass);
+            else hipLaunchKernelGGL((k_sort_scatter<2>), dim3(p.tiles + CLEAR), dim3(256), 0, st, a, 8 * pass);
+        }
     }
-    const uint32_t *key = a.key[p.passes & 1], *pos = a.pos[p.passes & 1];
+    const int last = p.bits ? 0 : p.passes & 1;
+    const uint32_t *key = a.key[last], *pos = a.pos[last];
     if (type == ACT_BF16) embed_sum<__bf16>(a, key, pos, st);
     else if (type == ACT_F16) embed_sum<_Float16>(a, key, pos, st);
     else embed_sum<float>(a, key, pos, st);

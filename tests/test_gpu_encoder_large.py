@@ -114,6 +114,20 @@ def test_convolution_in_longer_runs(B, T, C, W, ragged, dtype):
     assert far(gu[..., pick], ru) < tol and far(gw[pick], rw) < 2e-6 and far(gb[pick], rb) < 2e-6
 
 
+@pytest.mark.parametrize("n,V,D", [(1024, 1000, 8), (1025, 255, 8), (4096, 256, 16), (4097, 70000, 8), (4000, 1 << 21, 8),
+                                   (33000, 300, 8), (140_000, 66_000, 8)])
+def test_embedding_gradient_by_every_sort(n, V, D):
+    """One workgroup, few tiles, many tiles and long ones, one to three passes; whole numbers, whose sums are exact."""
+    print("[case] embed sort", n, V, D, flush=True)
+    g = torch.Generator(device=DEV).manual_seed(43)
+    tokens = (torch.rand(1, n, generator=g, device=DEV) ** 3 * V * 1.02).int()
+    tokens[0, ::13] = -5
+    grad = torch.randint(-8, 9, (1, n, D), generator=g, device=DEV).float()
+    valid = ((tokens >= 0) & (tokens < V))[0]
+    ref = torch.zeros(V, D, dtype=torch.float64, device=DEV).index_add_(0, tokens[0][valid].long(), grad[0][valid].double())
+    assert torch.equal(sb.semicrf_embed_bwd(tokens, grad, V).double(), ref)
+
+
 def test_nothing_is_read_before_it_is_written():
     """Workspaces and outputs full of not-a-numbers: the same bits as with fresh ones."""
     d, _ = make(3, 900, 4, 64, 2, 40, torch.bfloat16, [900, 0, 513], seed=37)
