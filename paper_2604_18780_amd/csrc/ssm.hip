@@ -78,15 +78,16 @@ __global__ __launch_bounds__(64) void k_ssm_chain(SsmArgs a, bool grad)
 //   across   from before the block to behind it.
 // The pairs that cross a boundary are known at a segment's ends (k_ssm_chain).  From the later one backwards, taking off those that
 // begin in a block leaves its `across`, and adding those that end in it gives what crosses its start.  Rounding adds up along that
-// walk, and all positions of a block share it: what the walk is off by at the segment's start is taken back in equal parts.
-// Where a block keeps less than 2^-30, nothing is left of the difference but rounding: `across` is 0, and the walk begins
-// anew.  One wave per (sequence, head, segment).
+// walk, and all positions of a block share it.  What the walk is off by at the segment's start is therefore taken back: each value
+// by the share that its variance has of the difference's, both ends' included, with the squares of what has been added up
+// (all of it rounded alike) as variances.  Where a block keeps less than 2^-30, nothing is left of the difference but rounding:
+// `across` is 0, and the walk begins anew.  One wave per (sequence, head, segment).
 constexpr int MOST_BLOCKS = 16;  // of a segment of 512
 
 template <class T> __global__ __launch_bounds__(64) void k_ssm_steps(SsmArgs a)
 {
     __shared__ double over[MOST_BLOCKS], qs[MOST_BLOCKS], rs[MOST_BLOCKS];
-    __shared__ float ks[MOST_BLOCKS];
+    __shared__ float ks[MOST_BLOCKS], q2[MOST_BLOCKS], r2[MOST_BLOCKS], var[MOST_BLOCKS];
     const int lane = threadIdx.x, Q = a.block, r = lane & (Q - 1);
     const int seg = blockIdx.x % a.nseg, bh = blockIdx.x / a.nseg, h = bh % a.H, b = bh / a.H;
     const int L = length_of(a.lengths, b, a.T);
@@ -102,9 +103,13 @@ template <class T> __global__ __launch_bounds__(64) void k_ssm_steps(SsmArgs a)
         const size_t at = (size_t)bh * a.T + t;
         double q = in ? (double)a.qint[at] : 0.0, ri = in ? (double)a.rint[at] : 0.0;
         float kept = in ? softplus((float)dts[t * a.dt_row] + bias) : 0.0f;
-        for (int d = 1; d < Q; d *= 2) q += __shfl_xor(q, d), ri += __shfl_xor(ri, d), kept += __shfl_xor(kept, d);
+        float qq = (float)(q * q), rr = (float)(ri * ri);
+        for (int d = 1; d < Q; d *= 2) {
+            q += __shfl_xor(q, d), ri += __shfl_xor(ri, d), kept += __shfl_xor(kept, d);
+            qq += __shfl_xor(qq, d), rr += __shfl_xor(rr, d);
+        }
         const int n = (i - t0 + lane) / Q;
-        if (r == 0 && n < nblk) qs[n] = q, rs[n] = ri, ks[n] = kept;
+        if (r == 0 && n < nblk) qs[n] = q, rs[n] = ri, ks[n] = kept, q2[n] = qq, r2[n] = rr;
     }
     double cross[2] = {0.0, 0.0};
     {
@@ -118,24 +123,27 @@ template <class T> __global__ __launch_bounds__(64) void k_ssm_steps(SsmArgs a)
     __syncthreads();
     {
         double across = cross[1];
-        int first = nblk;  // the walk's blocks: up to here
+        float spread = (float)(cross[1] * cross[1]);  // the walk's variance
+        int first = nblk;                             // its blocks: up to here
         for (int n = nblk - 1; n >= 0; --n) {
             const double qi = qs[n], ri = rs[n];
             const bool gone = ks[n] * rate * 1.44269504f < -30.0f;
-            const double off = gone ? across - qi : n == 0 ? across - qi + ri - cross[0] : 0.0;
             across -= qi;
-            if (lane == 0) over[n] = across;
+            spread += q2[n];
+            if (lane == 0) over[n] = across, var[n] = spread;
             if (gone || n == 0) {
-                // spread over the blocks from `first` down to this one: the later, the less of it has come together
+                const double off = gone ? across : across + ri - cross[0];
+                const float all = gone ? spread : spread + r2[n] + (float)(cross[0] * cross[0]);
                 __syncthreads();
-                const int m = first - n;
-                if (lane < m) over[n + lane] -= off * (double)(m - lane) / m;
+                if (lane < first - n && all > 0.0f) over[n + lane] -= off * (double)(var[n + lane] / all);
                 __syncthreads();
                 if (gone && lane == 0) over[n] = 0.0;
                 first = n;
                 across = 0.0;
+                spread = 0.0f;
             }
             across += ri;
+            spread += r2[n];
         }
     }
     __syncthreads();

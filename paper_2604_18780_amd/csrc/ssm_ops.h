@@ -28,13 +28,23 @@ template <> struct Parts<float> { static constexpr int raw = 3, made = 3; };
 template <int n> struct Op { bf8 p[n]; };
 
 // Two floats rounded to bfloat16 (to nearest even), the first in the lower half.
+typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t round2(float a, float b)
 {
-    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
     typedef float f2 __attribute__((ext_vector_type(2)));
     uint32_t o = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){a, b}, bf2));
     asm("" : "+v"(o));  // one conversion for the pair: without this each value is rounded again for its remainder
     return o;
+}
+// What rounding took from them: a product of the pair with (-1, 0), and with (0, -1), added to the value, which is exact and one
+// instruction where widening and subtracting are two.  The factors come as registers: as literals they are read wrongly.
+__device__ __forceinline__ void remainder2(uint32_t rounded, float &a, float &b)
+{
+    uint32_t first = 0x0000bf80u, second = 0xbf800000u;
+    asm("" : "+s"(first), "+s"(second));
+    const bf2 p = __builtin_bit_cast(bf2, rounded);
+    a = __builtin_amdgcn_fdot2_f32_bf16(p, __builtin_bit_cast(bf2, first), a, false);
+    b = __builtin_amdgcn_fdot2_f32_bf16(p, __builtin_bit_cast(bf2, second), b, false);
 }
 
 // n parts of 2 m values: v = p[0] + p[1] + ..
@@ -45,10 +55,7 @@ template <int n, int m> __device__ __forceinline__ void split_pairs(float (&v)[2
 #pragma unroll
         for (int k = 0; k < m; ++k) {
             o[i][k] = round2(v[2 * k], v[2 * k + 1]);
-            if (i + 1 < n) {
-                v[2 * k] -= __builtin_bit_cast(float, o[i][k] << 16);
-                v[2 * k + 1] -= __builtin_bit_cast(float, o[i][k] & 0xffff0000u);
-            }
+            if (i + 1 < n) remainder2(o[i][k], v[2 * k], v[2 * k + 1]);
         }
 }
 
