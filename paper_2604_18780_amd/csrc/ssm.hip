@@ -5,8 +5,7 @@ namespace semicrf_enc {
 
 // States at the segments' boundaries from what each segment adds: H_{s+1} = kept_s H_s + added_s forwards, and with `grad` the
 // same backwards for gradients of states, and the pairs of positions that cross each boundary: <G, H> there, by wave.  A
-// thread owns four entries, a workgroup is a wave, so that few heads still reach most of the chip; the loads of sixteen segments
-// are on their way at once.
+// thread owns four entries, and a workgroup is a wave, so that few heads still reach most of the chip.
 template <bool REV> __device__ __forceinline__ void chain_line(const SsmArgs &a, size_t bh, size_t at, bool mine, double *cross, size_t parts)
 {
     const size_t cells = (size_t)a.P * a.N;
@@ -14,33 +13,44 @@ template <bool REV> __device__ __forceinline__ void chain_line(const SsmArgs &a,
     const float *first = REV ? a.grad_last : a.state, *states = a.hs ? a.hs + bh * (a.nseg + 1) * cells + at : nullptr;
     float *last = REV ? a.gstate : a.state_out;
     const float *kept = a.kept + bh * a.nseg;
-    constexpr int AHEAD = REV ? 8 : 16;
+    constexpr int AHEAD = 8;
     f4 h = first && mine ? *(const f4 *)(first + bh * cells + at) : (f4)0.0f;
-    if (mine) *(f4 *)(line + (REV ? (size_t)a.nseg * cells : 0)) = h;
-    double pairs[AHEAD];
-    auto product = [&](f4 g, f4 h) { return (double)g[0] * h[0] + (double)g[1] * h[1] + (double)g[2] * h[2] + (double)g[3] * h[3]; };
-    auto put = [&](int boundary, double s) {
-        for (int d = 1; d < 64; d *= 2) s += __shfl_xor(s, d);
-        if (threadIdx.x == 0) cross[(bh * (a.nseg + 1) + boundary) * parts] = s;
-    };
-    if constexpr (REV) put(a.nseg, mine ? product(h, *(const f4 *)(states + (size_t)a.nseg * cells)) : 0.0);
-    for (int s0 = 0; s0 < a.nseg; s0 += AHEAD) {
-        f4 added[AHEAD], there[REV ? AHEAD : 1];
-        float k[AHEAD];
+    // the next eight segments' loads are on their way while eight are worked on
+    f4 added[AHEAD], there[REV ? AHEAD : 1], next[AHEAD], next_there[REV ? AHEAD : 1];
+    float k[AHEAD], next_k[AHEAD];
+    auto fetch = [&](int s0) {
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            added[i] = (f4)0.0f;
-            if constexpr (REV) there[i] = (f4)0.0f;
-            k[i] = 0.0f, pairs[i] = 0.0;
+            next[i] = (f4)0.0f;
+            if constexpr (REV) next_there[i] = (f4)0.0f;
+            next_k[i] = 0.0f;
             if (s0 + i < a.nseg && mine) {
                 const int s = REV ? a.nseg - 1 - s0 - i : s0 + i;
-                added[i] = *(const f4 *)(line + (size_t)(REV ? s : s + 1) * cells);
-                if constexpr (REV) there[i] = *(const f4 *)(states + (size_t)s * cells);
-                k[i] = kept[s];
+                next[i] = *(const f4 *)(line + (size_t)(REV ? s : s + 1) * cells);
+                if constexpr (REV) next_there[i] = *(const f4 *)(states + (size_t)s * cells);
+                next_k[i] = kept[s];
             }
         }
+    };
+    fetch(0);
+    auto product = [&](f4 g, f4 h) { return (double)g[0] * h[0] + (double)g[1] * h[1] + (double)g[2] * h[2] + (double)g[3] * h[3]; };
+    if constexpr (REV) {
+        double s = mine ? product(h, *(const f4 *)(states + (size_t)a.nseg * cells)) : 0.0;
+        for (int d = 1; d < 64; d *= 2) s += __shfl_xor(s, d);
+        if (threadIdx.x == 0) cross[(bh * (a.nseg + 1) + a.nseg) * parts] = s;
+    }
+    if (mine) *(f4 *)(line + (REV ? (size_t)a.nseg * cells : 0)) = h;
+    for (int s0 = 0; s0 < a.nseg; s0 += AHEAD) {
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
+            added[i] = next[i], k[i] = next_k[i];
+            if constexpr (REV) there[i] = next_there[i];
+        }
+        if (s0 + AHEAD < a.nseg) fetch(s0 + AHEAD);
+        double pairs[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            pairs[i] = 0.0;
             if (s0 + i < a.nseg) {
                 const int s = REV ? a.nseg - 1 - s0 - i : s0 + i;
                 h = k[i] * h + added[i];
