@@ -40,7 +40,7 @@ struct SsmArgs {
     float *kept;              // [B*H][nseg] what a state keeps over a segment
     float *partc, *partb;     // [chunks][B*T][G][N] gradients of C and B by workgroup, where there are several
     float *rint, *dlin, *qint, *xdu;  // [B*H][T] see k_ssm_steps
-    float *skipp;             // [B*H][nseg]
+    double *skipp;            // [B*H][nseg] sums for the skip
     double *cross;            // [B*H][nseg+1][P*N/256] pairs that cross a segment's boundary, by wave of k_ssm_chain
     double *headp;            // [B*H*nseg][2] sums for rate and bias
 };

@@ -201,7 +201,7 @@ __global__ __launch_bounds__(256) void k_ssm_params(SsmArgs a)
         const size_t at = ((size_t)(k / a.nseg) * a.H + h) * a.nseg + k % a.nseg;
         rate += a.headp[2 * at];
         bias += a.headp[2 * at + 1];
-        skip += (double)a.skipp[at];
+        skip += a.skipp[at];
     }
     s[0][tid] = rate, s[1][tid] = bias, s[2][tid] = skip;
     for (int d = 128; d > 0; d /= 2) {
@@ -398,7 +398,7 @@ int make_ssm_plan(int B, int T, int H, int P, int G, int N, bool grad, SsmPlan *
         p->dlin = take(rows * H * 4);
         p->qint = take(rows * H * 4);
         p->xdu = take(rows * H * 4);
-        p->skipp = take(bh * p->nseg * 4);
+        p->skipp = take(bh * p->nseg * 8);
         p->cross = take(bh * (p->nseg + 1) * ((cells / 4 + 63) / 64) * 8);
         p->headp = take(bh * p->nseg * 16);
     }
@@ -512,7 +512,7 @@ int semicrf_ssm_bwd(const void *x, int64_t x_row, const void *b, int64_t b_row, 
     a.hs = (float *)(w + p.hs); a.gs = (float *)(w + p.gs); a.kept = (float *)(w + p.kept);
     a.partc = (float *)(w + p.partc); a.partb = (float *)(w + p.partb);
     a.rint = (float *)(w + p.rint); a.dlin = (float *)(w + p.dlin); a.qint = (float *)(w + p.qint);
-    a.xdu = (float *)(w + p.xdu); a.skipp = (float *)(w + p.skipp); a.headp = (double *)(w + p.headp);
+    a.xdu = (float *)(w + p.xdu); a.skipp = (double *)(w + p.skipp); a.headp = (double *)(w + p.headp);
     a.cross = (double *)(w + p.cross);
     const hipStream_t st = (hipStream_t)stream;
     const int most = P > N ? P : N;

@@ -348,7 +348,7 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
     __bf16 *const sx = pool, *const sy = sx + TL::ELEMS, *const sb = sy + TL::ELEMS, *const sc = sb + TL::ELEMS, *const su = sc + TL::ELEMS,
         *const sm = su + SU::ELEMS, *const sg = sm + SC::ELEMS;  // sg: G [p][n]
     __shared__ __attribute__((aligned(16))) Steps<Q> ss[2][HB];
-    __shared__ float qp[2][NW][Q], xp[2][NW][Q];  // by wave: its columns' part of qint and x . du; of this head and the one before
+    __shared__ __attribute__((aligned(16))) float qp[2][NW][Q], xp[2][NW][Q];  // by wave: its columns' part of qint and x . du; of this head and the one before
 
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, i16 = lane & 15;
     const Place<T> at(a, HB, Q, a.chunks);
@@ -368,14 +368,15 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
 
     f4 S[HB][KT];                // G: rows n, this lane's column p
     f4 R[TWICE ? HB : 1][TWICE ? KT : 1];  // its transpose: rows p, this lane's column n
-    float rate[HB], bias[HB], skip[HB], skip_sum[HB];
+    float rate[HB], bias[HB], skip[HB];
+    double skip_sum[HB];
 #pragma unroll
     for (int k = 0; k < HB; ++k) {
         const int head = k < at.nh ? at.h0 + k : at.h0;
         rate[k] = a.rate[head];
         bias[k] = a.dt_bias ? a.dt_bias[head] : 0.0f;
         skip[k] = a.skip ? a.skip[head] : 0.0f;
-        skip_sum[k] = 0.0f;
+        skip_sum[k] = 0.0;
         const float *from = a.gs + ((size_t)(at.b * a.H + head) * (a.nseg + 1) + at.seg + 1) * cells;
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
@@ -508,8 +509,10 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
                 for (int ks = 0; ks < KS; ++ks)
                     p = mma_inputs(p, TL::by_row(sy, ln, jt, ks), TL::by_row(sx, ln, it, ks));
                 if (it == jt) {
+                    float on = 0.0f;  // the diagonal's
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) skip_sum[k] += 4 * g + r == i16 ? p[r] : 0.0f;
+                    for (int r = 0; r < 4; ++r) on += 4 * g + r == i16 ? p[r] : 0.0f;
+                    skip_sum[k] += (double)on;
                 }
 #pragma unroll
                 for (int o = 1; o < OWN; ++o)
@@ -610,12 +613,12 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
 #pragma unroll
     for (int k = 0; k < HB; ++k) {
         for (int d = 1; d < 64; d *= 2) skip_sum[k] += __shfl_xor(skip_sum[k], d);
-        if (lane == 0) qp[0][w][k] = skip_sum[k];
+        if (lane == 0) ((double *)qp[0][w])[k] = skip_sum[k];
     }
     lds_barrier();
     if (tid < at.nh) {
-        float s = 0.0f;
-        for (int y = 0; y < NW; ++y) s += qp[0][y][tid];
+        double s = 0.0;
+        for (int y = 0; y < NW; ++y) s += ((const double *)qp[0][y])[tid];
         a.skipp[(size_t)(at.b * a.H + at.h0 + tid) * a.nseg + at.seg] = s;
     }
     clear_rows<T>((T *)a.gx + at.rb * a.gx_row + at.h0 * a.P, a.gx_row, at.t0 + at.nblk * Q, at.t1, at.nh * a.P, tid, NT);
