@@ -9,6 +9,10 @@
 //   output  O[p,i] = sum_j x[j,p] M[j,i] + e^{c_i} sum_n S[n,p] C[i,n]
 //   state   S[n,p] = e^{c_Q} S[n,p] + sum_j B[j,n] (e^{c_Q-c_j} delta_j x[j,p])
 // Steps (delta, c) are made for four blocks at a time, one by each wave.
+//
+// Measured, bfloat16, 400 000 positions of 8 heads, 64 channels, 64 states: outputs 296 us, 922 MB (3.1 TB/s); states alone 129 us, 461 MB
+// (3.6 TB/s).  Bound by no unit: of the outputs' time the vector units are busy 45 %, LDS 55 % and the matrix cores 29 %; what is
+// left is the latency from one to the next with three waves on a SIMD (155 registers).
 #ifndef SEMICRF_SSM_FWD_INL
 #define SEMICRF_SSM_FWD_INL
 
