@@ -8,8 +8,8 @@
 // before or goes on in the next; those are joined in chunk order.  Zeros for tokens that do not occur are written while the
 // positions are sorted, which keeps few workgroups busy.  Bound by g read once and the table written once; for few tokens by the
 // launches: the sort's one, or two to three a pass, and two.
-// Measured, bfloat16: 4 x 100 000 tokens, table 4101 x 512, forwards 90 us (410 MB written, 4.6 TB/s), gradient 138 us, of which 91
-// add up rows (4.5 TB/s); 64 x 256 tokens, table 32000 x 512, gradient 40 us (65 MB of it zeros and sums).
+// Measured, bfloat16: 4 x 100 000 tokens, table 4101 x 512, forwards 72 us (410 MB written, 5.7 TB/s), gradient 130 us, of which 80
+// add up rows (5.1 TB/s); 64 x 256 tokens, table 32000 x 512, gradient 40 us (65 MB of it zeros and sums).
 #include "encoder.h"
 
 namespace semicrf_enc {
@@ -265,9 +265,10 @@ template <int R> __global__ __launch_bounds__(WIDE) void k_sort_whole(EmbedArgs 
     }
 }
 
-// One wave adds up one chunk of the sorted positions over 64 lanes of columns (91 us for 400 000 rows of 1 KB, 4.5 TB/s).  Keys and places are a lane's each, read once and
+// One wave adds up one chunk of the sorted positions over 64 lanes of columns (80 us for 400 000 rows of 1 KB, 5.1 TB/s).  Keys and places are a lane's each, read once and
 // handed round by lane, so that branches on them are the wave's and the rows of several positions are on their way at once.
-template <class T> __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs a, const uint32_t *key, const uint32_t *pos)
+// PAST: rows are read past the caches.
+template <class T, bool PAST> __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs a, const uint32_t *key, const uint32_t *pos)
 {
     constexpr int E = PER16<T>, AHEAD = 8;
     typedef T X __attribute__((ext_vector_type(E)));
@@ -290,7 +291,8 @@ template <class T> __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs 
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
             const int i = i0 + k < n ? i0 + k : n - 1;
-            next[k] = *(const X *)(g + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)at, i) * a.D);
+            const X *row = (const X *)(g + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)at, i) * a.D);
+            next[k] = PAST ? __builtin_nontemporal_load(row) : *row;
         }
     };
     fetch(0);
@@ -410,7 +412,12 @@ int embed_plan(int B, int T, int V, int D, EmbedPlan *p)
 template <class T> void embed_sum(const EmbedArgs &a, const uint32_t *key, const uint32_t *pos, hipStream_t st)
 {
     const int64_t waves = (int64_t)a.chunks * ((a.D + 64 * PER16<T> - 1) / (64 * PER16<T>));
-    hipLaunchKernelGGL((k_embed_sum<T>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, st, a, key, pos);
+    // Rows that the last-level cache (256 MB) hardly holds are read past it: 400 000 rows of 1 KB, forwards and gradient 203 us instead
+    // of 232; 16 384 rows 46 us, and 48 past it.
+    const bool past = (double)a.n * a.D * sizeof(T) > 128e6;
+    const dim3 g((unsigned)((waves + 3) / 4)), t(256);
+    if (past) hipLaunchKernelGGL((k_embed_sum<T, true>), g, t, 0, st, a, key, pos);
+    else hipLaunchKernelGGL((k_embed_sum<T, false>), g, t, 0, st, a, key, pos);
 }
 
 }  // namespace semicrf_enc

@@ -219,7 +219,8 @@ __global__ __launch_bounds__(256) void k_ssm_params(SsmArgs a)
 }
 
 // Gradients of B and C where several workgroups have parts: their sum, in order.  A thread owns four columns of a row.  Bound by the
-// parts: four of 400 000 rows of 64 and 64 columns, 922 MB in 181 us (5.1 TB/s).
+// parts: four of 400 000 rows of 64 and 64 columns, 922 MB in 157 us (5.9 TB/s; 181 where the parts
+// are read through the caches).
 template <class T> __global__ __launch_bounds__(256) void k_ssm_heads(SsmArgs a)
 {
     const int quads = a.N / 4;
@@ -230,7 +231,7 @@ template <class T> __global__ __launch_bounds__(256) void k_ssm_heads(SsmArgs a)
     const float *part = blockIdx.y ? a.partc : a.partb;
     f4 s = (f4)0.0f;
     if (t < length_of(a.lengths, b, a.T))
-        for (int k = 0; k < a.chunks; ++k) s += *(const f4 *)(part + ((int64_t)k * rows + row) * a.G * a.N + col);
+        for (int k = 0; k < a.chunks; ++k) s += __builtin_nontemporal_load((const f4 *)(part + ((int64_t)k * rows + row) * a.G * a.N + col));
     const float o[4] = {s[0], s[1], s[2], s[3]};
     store_n<T, 4>((T *)(blockIdx.y ? a.gc : a.gb) + row * (blockIdx.y ? a.gc_row : a.gb_row) + col, o);
 }
@@ -252,9 +253,10 @@ struct StepArgs {
 // needs for them: its channels of x and its group's B and C, again in every workgroup of the group (2 N W multiply-adds)
 // rather than in a launch before this one.  The ring holds the last W tokens at slot (position mod W), so the one slot that
 // is written is the one nobody reads.
-// Bound by the state, read and written once; its loads are on their way before the convolution starts: 192 streams of 16 heads of
-// 64 x 128 take 50 us (206 MB, 4.1 TB/s; 40 where the last-level cache holds it).  One stream takes 5 us, a launch and three loads that wait for one another.  Sixteen rows to a workgroup
-// spread one stream over the chip; where there are workgroups enough, 64 rows convolve B and C a quarter as often.
+// Bound by the state, read and written once and past the caches (51 us through them); its loads are on their way before the
+// convolution starts: 192 streams of 16 heads of 64 x 128 take 41 us (206 MB, 5.1 TB/s).  One stream takes 5 us, a launch and
+// three loads that wait for one another.  Sixteen rows to a workgroup spread one stream over the chip; where there are
+// workgroups enough, 64 rows convolve B and C a quarter as often.
 template <class T, int R> __global__ __launch_bounds__(256) void k_ssm_step(StepArgs a)
 {
     constexpr int ROWS = 16 * R;
@@ -270,7 +272,7 @@ template <class T, int R> __global__ __launch_bounds__(256) void k_ssm_step(Step
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             const int n = 4 * (q + 16 * k);
-            if (p0 + 16 * r < a.P && n < a.N) s[r][k] = *(const f4 *)(a.state + cell + (size_t)16 * r * a.N + n);
+            if (p0 + 16 * r < a.P && n < a.N) s[r][k] = __builtin_nontemporal_load((const f4 *)(a.state + cell + (size_t)16 * r * a.N + n));
         }
     const int seen = a.seen[b], W = a.W;
     const bool live = seen >= 0;
@@ -327,7 +329,7 @@ template <class T, int R> __global__ __launch_bounds__(256) void k_ssm_step(Step
                     const f4 m = s[r][k] * vc[k];
                     y += m[0] + m[1] + m[2] + m[3];
                 }
-                if (live || a.state_out != a.state) *(f4 *)(a.state_out + cell + (size_t)16 * r * a.N + n) = s[r][k];
+                if (live || a.state_out != a.state) __builtin_nontemporal_store(s[r][k], (f4 *)(a.state_out + cell + (size_t)16 * r * a.N + n));
             }
         }
 #pragma unroll
