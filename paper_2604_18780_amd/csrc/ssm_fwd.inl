@@ -36,6 +36,9 @@ __device__ __forceinline__ void scan_segment(const SsmArgs &a, unsigned block, S
     constexpr int NT = PV * 4, NW = PV / 16, KT = DK / 16, KS = DK / 32, IT = Q / 16, QS = Q / 32;
     constexpr int AHEAD = ScanShared<T, Q, DK, PV, OUT>::AHEAD;
     constexpr int RAW = Parts<T>::raw, MADE = Parts<T>::made, HELD = 3;
+    // queries are kept from the scores to the output, except where they would take 96 registers (float32, 128 states: 343 us so, 305
+    // read again; bfloat16 138 us kept, 154 read again; 16 x 4000 positions of 8 heads of 64)
+    constexpr bool HOLD = IT * KS * RAW <= 16;
     typedef Tile<T, Q, DK, NT, REV> TK;
     typedef Tile<T, Q, PV, NT, REV> TV;
     typedef Scores<Q, MADE> SC;
@@ -125,18 +128,24 @@ __device__ __forceinline__ void scan_segment(const SsmArgs &a, unsigned block, S
         if (n + 1 < nblk) fetch(n + 1);
         f4 O[IT];
         if constexpr (OUT) {
-            Op<RAW> q[IT][KS];
+            Op<RAW> held[HOLD ? IT : 1][HOLD ? KS : 1];
+            if constexpr (HOLD) {
 #pragma unroll
-            for (int it = 0; it < IT; ++it)
+                for (int it = 0; it < IT; ++it)
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) q[it][ks] = TK::by_row(sq, lk, it, ks);
+                    for (int ks = 0; ks < KS; ++ks) held[it][ks] = TK::by_row(sq, lk, it, ks);
+            }
+            auto q = [&](int it, int ks) -> Op<RAW> {
+                if constexpr (HOLD) return held[it][ks];
+                else return TK::by_row(sq, lk, it, ks);
+            };
 #pragma unroll
             for (int k = 0; k < SC::TILES; ++k) {
                 if (SC::wave(k, NW) != w) continue;
                 const int it = SC::query(k), jt = SC::keys(k);
                 f4 m = (f4)0.0f;
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) m = mma_inputs(m, TK::by_row(sk, lk, jt, ks), q[it][ks]);
+                for (int ks = 0; ks < KS; ++ks) m = mma_inputs(m, TK::by_row(sk, lk, jt, ks), q(it, ks));
                 m *= weights(s, it, jt, i16, g);
                 if (it == jt) m += skips;
                 SC::put(sm, it, jt, m, lane);
@@ -148,7 +157,7 @@ __device__ __forceinline__ void scan_segment(const SsmArgs &a, unsigned block, S
             for (int ks = 0; ks < KS; ++ks) {
                 const Op<MADE> st = split<MADE>(__builtin_shufflevector(S[2 * ks], S[2 * ks + 1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-                for (int it = 0; it < IT; ++it) O[it] = mma(O[it], st, q[it][ks]);
+                for (int it = 0; it < IT; ++it) O[it] = mma(O[it], st, q(it, ks));
             }
 #pragma unroll
             for (int it = 0; it < IT; ++it) O[it] *= s.out[16 * it + i16];
@@ -230,14 +239,22 @@ template <class T, int Q, int DK, int PV> int launch_scan(bool out, bool both, c
     else hipLaunchKernelGGL((k_ssm_states<T, Q, DK, PV>), dim3((unsigned)(both ? 2 * grid : grid)), t, 0, st, a, (unsigned)grid);
     return launched();
 }
+// Positions of a block: 64 as long as the staged parts leave room for two workgroups on a compute unit, and the rows on their way
+// take few of a thread's registers (narrow heads have few threads for as many rows of B and C).  16 x 4000 positions of 512
+// channels, with blocks of 64 and of 32: float32, heads of 32, 32 states 243 and 172 us; float16, heads of 16, 64 states 532 and
+// 303; bfloat16, heads of 32, 128 states 250 and 182, heads of 16, 64 states 210 and 232.
+template <class T> constexpr int scan_block(int DK, int PV)
+{
+    constexpr int R = Parts<T>::raw;
+    const int rows = 4 * (2 * DK + PV) * (int)sizeof(T) / PV;  // registers
+    return R * (2 * DK + PV) <= 448 && rows <= (R == 1 && DK <= 64 ? 72 : 40) ? 64 : 32;
+}
 template <class T, int DK> int launch_scan_p(bool out, bool both, const SsmArgs &a, hipStream_t st)
 {
-    // blocks of 64 as long as the staged parts leave room for two workgroups on a compute unit
-    constexpr int R = Parts<T>::raw;
-    if (a.P <= 16) return launch_scan<T, R * (2 * DK + 16) <= 448 ? 64 : 32, DK, 16>(out, both, a, st);
-    if (a.P <= 32) return launch_scan<T, R * (2 * DK + 32) <= 448 ? 64 : 32, DK, 32>(out, both, a, st);
-    if (a.P <= 64) return launch_scan<T, R * (2 * DK + 64) <= 448 ? 64 : 32, DK, 64>(out, both, a, st);
-    return launch_scan<T, R * (2 * DK + 128) <= 448 ? 64 : 32, DK, 128>(out, both, a, st);
+    if (a.P <= 16) return launch_scan<T, scan_block<T>(DK, 16), DK, 16>(out, both, a, st);
+    if (a.P <= 32) return launch_scan<T, scan_block<T>(DK, 32), DK, 32>(out, both, a, st);
+    if (a.P <= 64) return launch_scan<T, scan_block<T>(DK, 64), DK, 64>(out, both, a, st);
+    return launch_scan<T, scan_block<T>(DK, 128), DK, 128>(out, both, a, st);
 }
 template <class T> int ssm_scan(bool out, bool both, const SsmArgs &a, hipStream_t st)
 {
