@@ -28,7 +28,6 @@ struct SsmArgs {
     int B, T, H, P, G, N;
     int seg, nseg;            // positions of a segment (a multiple of 64) and how many there are
     int heads, chunks;        // heads of a group that a workgroup of the gradient kernels takes, and how many such there are
-    int block;                // positions of a block of the gradient kernels
     void *y;
     int64_t y_row;
     float *state_out;         // [B,H,P,N] or null
@@ -45,13 +44,12 @@ struct SsmArgs {
     double *headp;            // [B*H*nseg][2] sums for rate and bias
 };
 
-// Positions of a block of the gradient kernels, by the parts and the width of their four staged operands.  Blocks of 64 read a
-// state half as often, but want 250 registers, two waves to a SIMD, where blocks of 32 run three: 4 x 100 000 tokens, 8 heads of 64,
-// 64 states, bfloat16 took 611 + 1053 us with blocks of 64 and takes 485 + 627.
+// Positions of a block of the gradient kernels.  Blocks of 64 read a state half as often, but want 250 registers, two waves to a SIMD,
+// where blocks of 32 run three: 4 x 100 000 tokens, 8 heads of 64, 64 states, bfloat16 took 611 + 1053 us with blocks of 64 and takes
+// 485 + 627 (16 x 4000 tokens, 32 heads of 16, 32 states 910 and 575).
 // Heads that a workgroup of the gradient kernels takes where B and C are shared: one needs fewer registers, but leaves a part of the
 // gradients of B and C for each head (694 + 451 us and 331 to sum the parts, against 627 + 485 and 176), four spill.
-constexpr int GRAD_HEADS = 2;
-constexpr int grad_block(int raw, int dim) { return raw * dim <= 32 ? 64 : 32; }
+constexpr int GRAD_BLOCK = 32, GRAD_HEADS = 2;
 
 // One instantiation per storage type, each in a translation unit of its own: outputs, or states alone (forwards, or both ways in
 // one launch); and the gradient kernels.

@@ -100,7 +100,8 @@ template <class T> __global__ __launch_bounds__(64) void k_ssm_steps(SsmArgs a)
 {
     __shared__ double over[MOST_BLOCKS], qs[MOST_BLOCKS], rs[MOST_BLOCKS];
     __shared__ float ks[MOST_BLOCKS], q2[MOST_BLOCKS], r2[MOST_BLOCKS], var[MOST_BLOCKS];
-    const int lane = threadIdx.x, Q = a.block, r = lane & (Q - 1);
+    constexpr int Q = GRAD_BLOCK;
+    const int lane = threadIdx.x, r = lane & (Q - 1);
     const int seg = blockIdx.x % a.nseg, bh = blockIdx.x / a.nseg, h = bh % a.H, b = bh / a.H;
     const int L = length_of(a.lengths, b, a.T);
     const int t0 = seg * a.seg, t1 = t0 + a.seg < a.T ? t0 + a.seg : a.T;
@@ -108,7 +109,7 @@ template <class T> __global__ __launch_bounds__(64) void k_ssm_steps(SsmArgs a)
     T *gdt = (T *)a.gdt + (int64_t)b * a.T * a.gdt_row + h;
     const T *dts = (const T *)a.dt + (int64_t)b * a.T * a.dt_row + h;
     const float rate = a.rate[h], bias = a.dt_bias ? a.dt_bias[h] : 0.0f;
-    // sums of each block, 64 positions (two blocks of 32, or one of 64) at a time
+    // sums of each block, two blocks at a time
     for (int i = t0; i < end; i += 64) {
         const int t = i + lane;
         const bool in = t < end;
@@ -521,9 +522,7 @@ int semicrf_ssm_bwd(const void *x, int64_t x_row, const void *b, int64_t b_row, 
     a.xdu = (float *)(w + p.xdu); a.skipp = (double *)(w + p.skipp); a.headp = (double *)(w + p.headp);
     a.cross = (double *)(w + p.cross);
     const hipStream_t st = (hipStream_t)stream;
-    const int most = P > N ? P : N;
     a.heads = p.heads; a.chunks = p.chunks;
-    a.block = grad_block(type == ACT_F32 ? 3 : type == ACT_F16 ? 2 : 1, most <= 32 ? 32 : most <= 64 ? 64 : 128);
     if (int rc = scan(type, false, true, a, st)) return rc;
     if (int rc = chain(true, a, st)) return rc;
     if (int rc = grad(type, a, st)) return rc;

@@ -2,9 +2,9 @@
 // of x and B), each with what the gradients of the steps need on the way.
 //
 // A workgroup owns a segment and up to HB heads that share B and C; it takes a block's heads one after the other, so that rows of
-// B and C are staged once for all of them, C_i . B_j is formed once, and the sum over heads is a sum in registers.  A wave owns
-// sixteen of the 64 (32, 128) state columns: with P and N padded to the same DM, sixteen of N for the gradients of C and B,
-// sixteen of P for that of x.  Products, operands and steps as in ssm_fwd.inl.
+// B and C are staged once for all of them, C_i . B_j is formed once, and the sum over heads is a sum in registers.  P and N are
+// padded to PP and NN (32, 64, 128), and there is a wave to every sixteen of the wider: it owns sixteen columns of N for the
+// gradients of C and B, sixteen of P for that of x, where there are as many.  Products, operands and steps as in ssm_fwd.inl.
 //
 // Gradients of the steps: l_t multiplies every pair (i, j) with j < t <= i of W[i,j] = e^{c_i-c_j} (C_i . B_j) (dy_i . u_j).
 //   dlin[t]  pairs within t's block: sums of prefix and suffix sums of tiles of W, nothing subtracted
@@ -22,8 +22,9 @@
 
 namespace semicrf_enc {
 
-// Waves to a SIMD that the registers are cut for.
-constexpr int waves_for(int raw, int Q, int DM) { return Q == 32 && DM <= 64 && raw == 1 ? 3 : 2; }
+// Waves to a SIMD that the registers are cut for (16 x 4000 positions, 8 heads of 64, 64 states, float16: 475 us with two, 439 with
+// three; what is wider spills).
+constexpr int waves_for(int raw, int most) { return most <= 64 && raw <= 2 ? 3 : 2; }
 
 // What both kernels know of their workgroup.
 template <class T> struct Place {
@@ -112,17 +113,19 @@ template <class T> __device__ __forceinline__ void clear_rows(T *out, int64_t ro
 
 // ---- gradient of C ------------------------------------------------------------------------------------------------
 //   dC_i = sum_h sum_{j<=i} e^{c_i-c_j} (dy_i . u_j) B_j:  queries dy, keys x (scaled by delta), values B; state H [P x N]
-template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, waves_for(Parts<T>::raw, Q, DM)) void k_ssm_grad_c(SsmArgs a)
+template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN ? PP : NN) * 4, waves_for(Parts<T>::raw, PP > NN ? PP : NN)) void k_ssm_grad_c(SsmArgs a)
 {
-    constexpr int NT = DM * 4, NW = DM / 16, KT = DM / 16, KS = DM / 32, IT = Q / 16, QS = Q / 32;
+    constexpr int Q = GRAD_BLOCK, MOST = PP > NN ? PP : NN, NT = MOST * 4, NW = MOST / 16, IT = Q / 16, QS = Q / 32;
+    constexpr int KTP = PP / 16, KTN = NN / 16, KSP = PP / 32, KSN = NN / 32;
     constexpr int RAW = Parts<T>::raw, MADE = Parts<T>::made, HELD = 3, E = (int)sizeof(T);
-    typedef Tile<T, Q, DM, NT, false> TL;
+    typedef Tile<T, Q, PP, NT, false> TP;
+    typedef Tile<T, Q, NN, NT, false> TN;
     typedef Scores<Q, MADE> SC;
     constexpr int OWN = (SC::TILES + NW - 1) / NW;  // tiles of scores a wave makes at most
     constexpr int TURNS = (IT + NW - 1) / NW;       // sixteens of positions whose sums a wave makes
     // one array, so that operands' places differ by constants
-    __shared__ __attribute__((aligned(16))) __bf16 pool[4 * TL::ELEMS + SC::ELEMS];
-    __bf16 *const sx = pool, *const sy = sx + TL::ELEMS, *const sb = sy + TL::ELEMS, *const sc = sb + TL::ELEMS, *const sm = sc + TL::ELEMS;
+    __shared__ __attribute__((aligned(16))) __bf16 pool[2 * TP::ELEMS + 2 * TN::ELEMS + SC::ELEMS];
+    __bf16 *const sx = pool, *const sy = sx + TP::ELEMS, *const sb = sy + TP::ELEMS, *const sc = sb + TN::ELEMS, *const sm = sc + TN::ELEMS;
     __shared__ __attribute__((aligned(16))) Steps<Q> ss[2][HB];
     __shared__ float rp[NW][Q];             // by wave: its columns' part of rint
     __shared__ float ends[SC::TILES][16];   // sums of a tile of W by its later positions (on the diagonal: dlin), ..
@@ -133,17 +136,21 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
     if (!at.any) return;
     const size_t cells = (size_t)a.P * a.N;
     const int n0 = 16 * w + i16;  // this lane's column of the state
+    const bool own_n = NN == MOST || 16 * w < NN;
 
     Sources<T> src(a, at, at.t0);
-    TL rx, ry, rbt, rct;
-    const typename TL::Lane ln(lane, w);
-    const typename TL::Place pl(tid);
+    TP rx, ry;
+    TN rbt, rct;
+    const typename TP::Lane lp(lane, w);
+    const typename TN::Lane ln(lane, w);
+    const typename TP::Place plp(tid);
+    const typename TN::Place pln(tid);
     rx.init(src.x_bytes, a.P, tid);
     ry.init(src.y_bytes, a.P, tid);
     rbt.init(src.b_bytes, a.N, tid);
     rct.init(src.c_bytes, a.N, tid);
 
-    f4 S[HB][KT];
+    f4 S[HB][KTP];
     float rate[HB], bias[HB];
 #pragma unroll
     for (int k = 0; k < HB; ++k) {
@@ -152,7 +159,7 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
         bias[k] = a.dt_bias ? a.dt_bias[head] : 0.0f;
         const float *from = a.hs + ((size_t)(at.b * a.H + head) * (a.nseg + 1) + at.seg) * cells;
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
+        for (int kt = 0; kt < KTP; ++kt) {
             S[k][kt] = (f4)0.0f;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
@@ -182,8 +189,8 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
     const SharedOut<T> out(a, a.gc, a.gc_row, a.partc, a.chunks, at);
     for (int n = 0; n < at.nblk; ++n) {
         const int base = at.t0 + Q * n;
-        rbt.put(sb, pl, tid);
-        rct.put(sc, pl, tid);
+        rbt.put(sb, pln, tid);
+        rct.put(sc, pln, tid);
         Op<RAW> v[QS];
         f4 O[IT], D[OWN];
 #pragma unroll
@@ -191,8 +198,8 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
 #pragma unroll
         for (int k = 0; k < HB; ++k) {
             if (k >= at.nh) break;
-            rx.put(sx, pl, tid);
-            ry.put(sy, pl, tid);
+            rx.put(sx, plp, tid);
+            ry.put(sy, plp, tid);
             lds_barrier();
             // the next head's rows, or the next block's
             {
@@ -208,15 +215,15 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
             }
             if (k == 0) {
 #pragma unroll
-                for (int ks = 0; ks < QS; ++ks) v[ks] = TL::own_col(sb, ln, ks);
+                for (int ks = 0; ks < QS; ++ks) v[ks] = TN::own_col(sb, ln, ks);
                 int own = 0;
 #pragma unroll
                 for (int m = 0; m < SC::TILES; ++m) {
                     if (SC::wave(m, NW) != w) continue;
                     f4 d = (f4)0.0f;
 #pragma unroll
-                    for (int ks = 0; ks < KS; ++ks)
-                        d = mma_inputs(d, TL::by_row(sb, ln, SC::keys(m), ks), TL::by_row(sc, ln, SC::query(m), ks));
+                    for (int ks = 0; ks < KSN; ++ks)
+                        d = mma_inputs(d, TN::by_row(sb, ln, SC::keys(m), ks), TN::by_row(sc, ln, SC::query(m), ks));
 #pragma unroll
                     for (int o = 0; o < OWN; ++o)
                         if (o == own) D[o] = d;
@@ -231,8 +238,8 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
                 const int it = SC::query(m), jt = SC::keys(m);
                 f4 p = (f4)0.0f, d = D[0];
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks)
-                    p = mma_inputs(p, TL::by_row(sx, ln, jt, ks), TL::by_row(sy, ln, it, ks));
+                for (int ks = 0; ks < KSP; ++ks)
+                    p = mma_inputs(p, TP::by_row(sx, lp, jt, ks), TP::by_row(sy, lp, it, ks));
                 p *= weights(s, it, jt, i16, g);
                 SC::put(sm, it, jt, p, lane);
 #pragma unroll
@@ -263,42 +270,45 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
             }
             if (w == NW - 1) make_steps<Q, false>(ss[(n + 1) & 1][k], dt[k].value(), bias[k], rate[k], true, lane);
             fetch_dt(n + 2, k);
-            // what the state at the block's start gives
-            f4 F[IT];
+            if (own_n) {
+                // what the state at the block's start gives
+                f4 F[IT];
 #pragma unroll
-            for (int it = 0; it < IT; ++it) F[it] = (f4)0.0f;
+                for (int it = 0; it < IT; ++it) F[it] = (f4)0.0f;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const Op<HELD> st = split<HELD>(__builtin_shufflevector(S[k][2 * ks], S[k][2 * ks + 1], 0, 1, 2, 3, 4, 5, 6, 7));
+                for (int ks = 0; ks < KSP; ++ks) {
+                    const Op<HELD> st = split<HELD>(__builtin_shufflevector(S[k][2 * ks], S[k][2 * ks + 1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-                for (int it = 0; it < IT; ++it) F[it] = mma(F[it], st, TL::by_row(sy, ln, it, ks));
-            }
+                    for (int it = 0; it < IT; ++it) F[it] = mma(F[it], st, TP::by_row(sy, lp, it, ks));
+                }
 #pragma unroll
-            for (int it = 0; it < IT; ++it) {
-                F[it] *= s.out[16 * it + i16];
-                const f4 e = F[it] * TL::four(sc, ln, it);
-                const float sum = sum_rows(e[0] + e[1] + e[2] + e[3]);
-                if (g == 0) rp[w][16 * it + i16] = sum;
-                O[it] += F[it];
-            }
-            // the state at the block's end
-            {
-                const float keep = pow2(s.total);
+                for (int it = 0; it < IT; ++it) {
+                    F[it] *= s.out[16 * it + i16];
+                    const f4 e = F[it] * TN::four(sc, ln, it);
+                    const float sum = sum_rows(e[0] + e[1] + e[2] + e[3]);
+                    if (g == 0) rp[w][16 * it + i16] = sum;
+                    O[it] += F[it];
+                }
+                // the state at the block's end
+                {
+                    const float keep = pow2(s.total);
 #pragma unroll
-                for (int kt = 0; kt < KT; ++kt) S[k][kt] *= keep;
+                    for (int kt = 0; kt < KTP; ++kt) S[k][kt] *= keep;
 #pragma unroll
-                for (int ks = 0; ks < QS; ++ks) {
-                    const f4 lo = *(const f4 *)(s.in + 32 * ks + 4 * g), hi = *(const f4 *)(s.in + 32 * ks + 16 + 4 * g);
-                    const Op<HELD> u = split<HELD>(values(v[ks]) * __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                    for (int ks = 0; ks < QS; ++ks) {
+                        const f4 lo = *(const f4 *)(s.in + 32 * ks + 4 * g), hi = *(const f4 *)(s.in + 32 * ks + 16 + 4 * g);
+                        const Op<HELD> u = split<HELD>(values(v[ks]) * __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-                    for (int kt = 0; kt < KT; ++kt) S[k][kt] = mma(S[k][kt], TL::by_col(sx, ln, ks, kt), u);
+                        for (int kt = 0; kt < KTP; ++kt) S[k][kt] = mma(S[k][kt], TP::by_col(sx, lp, ks, kt), u);
+                    }
                 }
             }
             lds_barrier();
 #pragma unroll
             for (int it = 0; it < IT; ++it)
 #pragma unroll
-                for (int ks = 0; ks <= it / 2; ++ks) O[it] = mma(O[it], v[ks], SC::get(sm, SC::op(it, ks), lane));
+                for (int ks = 0; ks <= it / 2; ++ks)
+                    if (own_n) O[it] = mma(O[it], v[ks], SC::get(sm, SC::op(it, ks), lane));
             // sums over waves and tiles: each wave those of its sixteens, lane = position
             const size_t line = (size_t)(at.b * a.H + at.h0 + k) * a.T;
 #pragma unroll
@@ -307,7 +317,7 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
                 float ri = 0.0f, dl = 0.0f;
                 if (K < IT) {
                     float before = 0.0f, after = 0.0f;
-                    for (int x = 0; x < NW; ++x) ri += rp[x][at16];
+                    for (int x = 0; x < KTN; ++x) ri += rp[x][at16];
 #pragma unroll
                     for (int m = 0; m < SC::TILES; ++m) {
                         const int it = SC::query(m), jt = SC::keys(m);
@@ -338,18 +348,20 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
 // Rows run backwards in time.  A wave holds sixteen columns p of G; its parts, which the product with B needs anyway, go through
 // LDS, from where they are read transposed for the product with x.  Only float32 at a width of 128 has no room for that (98 KB):
 // there a wave holds sixteen columns n of the transpose as well, at twice the products for the updates.
-template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, waves_for(Parts<T>::raw, Q, DM)) void k_ssm_grad_xb(SsmArgs a)
+template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN ? PP : NN) * 4, waves_for(Parts<T>::raw, PP > NN ? PP : NN)) void k_ssm_grad_xb(SsmArgs a)
 {
-    constexpr int NT = DM * 4, NW = DM / 16, KT = DM / 16, KS = DM / 32, IT = Q / 16, QS = Q / 32;
+    constexpr int Q = GRAD_BLOCK, MOST = PP > NN ? PP : NN, NT = MOST * 4, NW = MOST / 16, IT = Q / 16, QS = Q / 32;
+    constexpr int KTP = PP / 16, KTN = NN / 16, KSP = PP / 32, KSN = NN / 32;
     constexpr int RAW = Parts<T>::raw, MADE = Parts<T>::made, HELD = 3, E = (int)sizeof(T);
-    typedef Tile<T, Q, DM, NT, true> TL;
+    typedef Tile<T, Q, PP, NT, true> TP;
+    typedef Tile<T, Q, NN, NT, true> TN;
     typedef Scores<Q, HELD> SU;  // for the gradient of u, which goes into those of the steps as well
     typedef Scores<Q, MADE> SC;
     constexpr int OWN = (SC::TILES + NW - 1) / NW, TURNS = (IT + NW - 1) / NW;
-    constexpr bool TWICE = RAW == 3 && DM == 128;
+    constexpr bool TWICE = RAW == 3 && PP == 128 && NN == 128;
     // one array, so that operands' places differ by constants
-    __shared__ __attribute__((aligned(16))) __bf16 pool[4 * TL::ELEMS + SU::ELEMS + SC::ELEMS + (TWICE ? 0 : MADE * DM * DM)];
-    __bf16 *const sx = pool, *const sy = sx + TL::ELEMS, *const sb = sy + TL::ELEMS, *const sc = sb + TL::ELEMS, *const su = sc + TL::ELEMS,
+    __shared__ __attribute__((aligned(16))) __bf16 pool[2 * TP::ELEMS + 2 * TN::ELEMS + SU::ELEMS + SC::ELEMS + (TWICE ? 0 : MADE * PP * NN)];
+    __bf16 *const sx = pool, *const sy = sx + TP::ELEMS, *const sb = sy + TP::ELEMS, *const sc = sb + TN::ELEMS, *const su = sc + TN::ELEMS,
         *const sm = su + SU::ELEMS, *const sg = sm + SC::ELEMS;  // sg: G [p][n]
     __shared__ __attribute__((aligned(16))) Steps<Q> ss[2][HB];
     __shared__ __attribute__((aligned(16))) float qp[2][NW][Q], xp[2][NW][Q];  // by wave: its columns' part of qint and x . du; of this head and the one before
@@ -358,20 +370,27 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
     const Place<T> at(a, HB, Q, a.chunks);
     if (!at.any) return;
     const size_t cells = (size_t)a.P * a.N;
-    const int c0 = 16 * w + i16;  // this lane's column
+    // Where there are more waves than columns of P, some hold the same ones, and only the first of them write: without a branch the
+    // compiler finds the registers (8 x 4000 positions, 8 heads of 64, 128 states: bfloat16 390 us, 437 with one, 420 with P padded
+    // to 128 as well).  Columns of N are few enough to be branched on.
+    const int wp = w % KTP, c0 = 16 * wp + i16, n0 = 16 * w + i16;  // this lane's columns
+    const bool own_n = NN == MOST || 16 * w < NN;
 
     auto base_of = [&](int n) { return at.t0 + Q * (at.nblk - 1 - n); };
     Sources<T> src(a, at, at.nblk ? base_of(0) : at.t0);
-    TL rx, ry, rbt, rct;
-    const typename TL::Lane ln(lane, w);
-    const typename TL::Place pl(tid);
+    TP rx, ry;
+    TN rbt, rct;
+    const typename TP::Lane lp(lane, wp);
+    const typename TN::Lane ln(lane, w);
+    const typename TP::Place plp(tid);
+    const typename TN::Place pln(tid);
     rx.init(src.x_bytes, a.P, tid);
     ry.init(src.y_bytes, a.P, tid);
     rbt.init(src.b_bytes, a.N, tid);
     rct.init(src.c_bytes, a.N, tid);
 
-    f4 S[HB][KT];                // G: rows n, this lane's column p
-    f4 R[TWICE ? HB : 1][TWICE ? KT : 1];  // its transpose: rows p, this lane's column n
+    f4 S[HB][KTN];               // G: rows n, this lane's column p
+    f4 R[TWICE ? HB : 1][TWICE ? KTP : 1];  // its transpose: rows p, this lane's column n
     float rate[HB], bias[HB], skip[HB];
     double skip_sum[HB];
 #pragma unroll
@@ -383,14 +402,14 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
         skip_sum[k] = 0.0;
         const float *from = a.gs + ((size_t)(at.b * a.H + head) * (a.nseg + 1) + at.seg + 1) * cells;
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
+        for (int kt = 0; kt < KTN; ++kt) {
             const int row = 16 * kt + 4 * g;
             S[k][kt] = at.nblk && row < a.N && c0 < a.P ? *(const f4 *)(from + (size_t)c0 * a.N + row) : (f4)0.0f;
             if constexpr (TWICE) {
                 R[k][kt] = (f4)0.0f;
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    if (at.nblk && row + r < a.P && c0 < a.N) R[k][kt][r] = from[(size_t)(row + r) * a.N + c0];
+                    if (at.nblk && row + r < a.P && n0 < a.N) R[k][kt][r] = from[(size_t)(row + r) * a.N + n0];
             }
         }
     }
@@ -428,15 +447,15 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
             const int K = w + NW * x, at16 = 16 * K + i16;
             float q = 0.0f, s = 0.0f;
             if (K < IT)
-                for (int y = 0; y < NW; ++y) q += qp[p][y][at16], s += xp[p][y][at16];
+                for (int y = 0; y < KTP; ++y) q += qp[p][y][at16], s += xp[p][y][at16];
             put_line<Q>(a.qint + line, base, at.t1, any && K < IT && g == 0 ? Q - 1 - at16 : -1, q);
             put_line<Q>(a.xdu + line, base, at.t1, any && K < IT && g == 0 ? Q - 1 - at16 : -1, s);
         }
     };
     for (int n = 0; n < at.nblk; ++n) {
         const int base = base_of(n);
-        rbt.put(sb, pl, tid);
-        rct.put(sc, pl, tid);
+        rbt.put(sb, pln, tid);
+        rct.put(sc, pln, tid);
         Op<RAW> vc[QS];
         f4 O[IT], D[OWN];
 #pragma unroll
@@ -444,19 +463,19 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
 #pragma unroll
         for (int k = 0; k < HB; ++k) {
             if (k >= at.nh) break;
-            rx.put(sx, pl, tid);
-            ry.put(sy, pl, tid);
-            Op<HELD> st[KS];
+            rx.put(sx, plp, tid);
+            ry.put(sy, plp, tid);
+            Op<HELD> st[KSN];
             {
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
+                for (int ks = 0; ks < KSN; ++ks) {
                     st[ks] = split<HELD>(__builtin_shufflevector(S[k][2 * ks], S[k][2 * ks + 1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
                     for (int part = 0; part < (TWICE ? 0 : MADE); ++part) {
                         const u4 v = __builtin_bit_cast(u4, st[ks].p[part]);
-                        __bf16 *to = sg + part * DM * DM + 16 * w * DM + ks / 2 * 64;
-                        *(u2 *)(to + ln.row[DM >= 64 ? ks % 2 * 2 : 0]) = (u2){v[0], v[1]};
-                        *(u2 *)(to + ln.row[DM >= 64 ? ks % 2 * 2 + 1 : 1]) = (u2){v[2], v[3]};
+                        __bf16 *to = sg + part * PP * NN + 16 * wp * NN + ks / 2 * 64;
+                        *(u2 *)(to + ln.row[NN >= 64 ? ks % 2 * 2 : 0]) = (u2){v[0], v[1]};
+                        *(u2 *)(to + ln.row[NN >= 64 ? ks % 2 * 2 + 1 : 1]) = (u2){v[2], v[3]};
                     }
                 }
             }
@@ -478,15 +497,15 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
             else join(n, k - 1, true);
             if (k == 0) {
 #pragma unroll
-                for (int ks = 0; ks < QS; ++ks) vc[ks] = TL::own_col(sc, ln, ks);
+                for (int ks = 0; ks < QS; ++ks) vc[ks] = TN::own_col(sc, ln, ks);
                 int own = 0;
 #pragma unroll
                 for (int m = 0; m < SC::TILES; ++m) {
                     if (SC::wave(m, NW) != w) continue;
                     f4 d = (f4)0.0f;
 #pragma unroll
-                    for (int ks = 0; ks < KS; ++ks)
-                        d = mma_inputs(d, TL::by_row(sc, ln, SC::keys(m), ks), TL::by_row(sb, ln, SC::query(m), ks));
+                    for (int ks = 0; ks < KSN; ++ks)
+                        d = mma_inputs(d, TN::by_row(sc, ln, SC::keys(m), ks), TN::by_row(sb, ln, SC::query(m), ks));
 #pragma unroll
                     for (int o = 0; o < OWN; ++o)
                         if (o == own) D[o] = d;
@@ -495,14 +514,12 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
             }
             const Steps<Q> &s = ss[n & 1][k];
             f4 U[IT];
-            {
 #pragma unroll
-                for (int it = 0; it < IT; ++it) U[it] = (f4)0.0f;
+            for (int it = 0; it < IT; ++it) U[it] = (f4)0.0f;
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks)
+            for (int ks = 0; ks < KSN; ++ks)
 #pragma unroll
-                    for (int it = 0; it < IT; ++it) U[it] = mma(U[it], st[ks], TL::by_row(sb, ln, it, ks));
-            }
+                for (int it = 0; it < IT; ++it) U[it] = mma(U[it], st[ks], TN::by_row(sb, ln, it, ks));
             int own = 0;
 #pragma unroll
             for (int m = 0; m < SC::TILES; ++m) {
@@ -510,8 +527,8 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
                 const int it = SC::query(m), jt = SC::keys(m);
                 f4 p = (f4)0.0f, d = D[0];
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks)
-                    p = mma_inputs(p, TL::by_row(sy, ln, jt, ks), TL::by_row(sx, ln, it, ks));
+                for (int ks = 0; ks < KSP; ++ks)
+                    p = mma_inputs(p, TP::by_row(sy, lp, jt, ks), TP::by_row(sx, lp, it, ks));
                 if (it == jt) {
                     float on = 0.0f;  // the diagonal's
 #pragma unroll
@@ -529,17 +546,17 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
             if (w == NW - 1) make_steps<Q, true>(ss[(n + 1) & 1][k], dt[k].value(), bias[k], rate[k], false, lane);
             fetch_dt(n + 2, k);
             // what the state behind the block gives to the gradient of B ..
-            {
+            if (own_n) {
                 f4 F[IT];
 #pragma unroll
                 for (int it = 0; it < IT; ++it) F[it] = (f4)0.0f;
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
+                for (int ks = 0; ks < KSP; ++ks) {
                     Op<MADE> gt;
                     if constexpr (TWICE) gt = split<MADE>(__builtin_shufflevector(R[k][2 * ks], R[k][2 * ks + 1], 0, 1, 2, 3, 4, 5, 6, 7));
-                    else gt = TL::template transposed<MADE>(sg, ln.own, 32 * ks * DM, DM * DM);
+                    else gt = TN::template transposed<MADE>(sg, ln.own, 32 * ks * NN, PP * NN);
 #pragma unroll
-                    for (int it = 0; it < IT; ++it) F[it] = mma(F[it], gt, TL::by_row(sx, ln, it, ks));
+                    for (int it = 0; it < IT; ++it) F[it] = mma(F[it], gt, TP::by_row(sx, lp, it, ks));
                 }
 #pragma unroll
                 for (int it = 0; it < IT; ++it) O[it] += F[it] * (s.out[16 * it + i16] * s.delta[16 * it + i16]);
@@ -547,43 +564,38 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
             // .. and to that of u
             f4 xv[IT], yv[IT];
             Op<RAW> vy[QS];
-            {
 #pragma unroll
-                for (int ks = 0; ks < QS; ++ks) vy[ks] = TL::own_col(sy, ln, ks);
-            }
+            for (int ks = 0; ks < QS; ++ks) vy[ks] = TP::own_col(sy, lp, ks);
 #pragma unroll
             for (int it = 0; it < IT; ++it) {
-                float sum = 0.0f;
-                {
-                    U[it] *= s.out[16 * it + i16];
-                    xv[it] = TL::four(sx, ln, it);
-                    yv[it] = TL::four(sy, ln, it);
-                    const f4 e = U[it] * xv[it];
-                    sum = sum_rows(e[0] + e[1] + e[2] + e[3]);
-                }
+                U[it] *= s.out[16 * it + i16];
+                xv[it] = TP::four(sx, lp, it);
+                yv[it] = TP::four(sy, lp, it);
+                const f4 e = U[it] * xv[it];
+                const float sum = sum_rows(e[0] + e[1] + e[2] + e[3]);
                 if (g == 0) qp[turn & 1][w][16 * it + i16] = sum * s.delta[16 * it + i16];
             }
             // the state before the block
             {
                 const float keep = pow2(s.total);
 #pragma unroll
-                for (int kt = 0; kt < KT; ++kt) S[k][kt] *= keep;
+                for (int kt = 0; kt < KTN; ++kt) S[k][kt] *= keep;
 #pragma unroll
                 for (int ks = 0; ks < QS; ++ks) {
                     const f4 lo = *(const f4 *)(s.in + 32 * ks + 4 * g), hi = *(const f4 *)(s.in + 32 * ks + 16 + 4 * g);
                     const f8 in = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
                     const Op<HELD> u = split<HELD>(values(vy[ks]) * in);
 #pragma unroll
-                    for (int kt = 0; kt < KT; ++kt) S[k][kt] = mma(S[k][kt], TL::by_col(sc, ln, ks, kt), u);
+                    for (int kt = 0; kt < KTN; ++kt) S[k][kt] = mma(S[k][kt], TN::by_col(sc, ln, ks, kt), u);
                     if constexpr (TWICE) {
                         const Op<MADE> v = split<MADE>(values(vc[ks]) * in);
 #pragma unroll
-                        for (int kt = 0; kt < KT; ++kt) R[k][kt] = mma(ks ? R[k][kt] : R[k][kt] * keep, TL::by_col(sy, ln, ks, kt), v);
+                        for (int kt = 0; kt < KTP; ++kt) R[k][kt] = mma(ks ? R[k][kt] : R[k][kt] * keep, TP::by_col(sy, lp, ks, kt), v);
                     }
                 }
             }
             lds_barrier();
-            {
+            if (own_n) {
 #pragma unroll
                 for (int it = 0; it < IT; ++it)
 #pragma unroll
@@ -592,15 +604,10 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
 #pragma unroll
             for (int it = 0; it < IT; ++it) {
                 const int r = 16 * it + i16;
-                float sum = 0.0f;
-                f4 o = (f4)0.0f;
-                {
 #pragma unroll
-                    for (int ks = 0; ks <= it / 2; ++ks) U[it] = mma(U[it], vy[ks], SU::get(su, SU::op(it, ks), lane));
-                    const f4 e = U[it] * xv[it];
-                    o = U[it] * s.delta[r] + yv[it] * skip[k];
-                    sum = sum_rows(e[0] + e[1] + e[2] + e[3]);
-                }
+                for (int ks = 0; ks <= it / 2; ++ks) U[it] = mma(U[it], vy[ks], SU::get(su, SU::op(it, ks), lane));
+                const f4 e = U[it] * xv[it], o = U[it] * s.delta[r] + yv[it] * skip[k];
+                const float sum = sum_rows(e[0] + e[1] + e[2] + e[3]);
                 if (g == 0) xp[turn & 1][w][r] = sum;
                 store_four<T>(rows_at(gxs, at.t1 - base, Q, gx_bytes), gx_off, 16 * (IT - 1 - it) * gx_bytes + k * a.P * E, o);
             }
@@ -630,28 +637,32 @@ template <class T, int Q, int DM, int HB> __global__ __launch_bounds__(DM * 4, w
         clear_rows<T>((T *)a.gb + at.rb * a.gb_row + at.grp * a.N, a.gb_row, at.t0 + at.nblk * Q, at.t1, a.N, tid, NT);
 }
 
-template <class T, int Q, int DM> int launch_grad(const SsmArgs &a, hipStream_t st)
+template <class T, int PP, int NN> int launch_grad(const SsmArgs &a, hipStream_t st)
 {
+    constexpr int MOST = PP > NN ? PP : NN, HB = MOST <= 64 ? GRAD_HEADS : 1;
     const long grid = ((long)a.B * a.nseg + 7) / 8 * 8 * a.G * a.chunks;
     if (grid > 0x7fffffffL) return SEMICRF_EUNSUPPORTED;
-    const dim3 g((unsigned)grid), t(DM * 4);
-    constexpr int HB = DM <= 64 ? GRAD_HEADS : 1;
+    const dim3 g((unsigned)grid), t(MOST * 4);
     if (a.heads > 1) {
-        hipLaunchKernelGGL((k_ssm_grad_c<T, Q, DM, HB>), g, t, 0, st, a);
-        hipLaunchKernelGGL((k_ssm_grad_xb<T, Q, DM, HB>), g, t, 0, st, a);
+        hipLaunchKernelGGL((k_ssm_grad_c<T, PP, NN, HB>), g, t, 0, st, a);
+        hipLaunchKernelGGL((k_ssm_grad_xb<T, PP, NN, HB>), g, t, 0, st, a);
     } else {
-        hipLaunchKernelGGL((k_ssm_grad_c<T, Q, DM, 1>), g, t, 0, st, a);
-        hipLaunchKernelGGL((k_ssm_grad_xb<T, Q, DM, 1>), g, t, 0, st, a);
+        hipLaunchKernelGGL((k_ssm_grad_c<T, PP, NN, 1>), g, t, 0, st, a);
+        hipLaunchKernelGGL((k_ssm_grad_xb<T, PP, NN, 1>), g, t, 0, st, a);
     }
     return launched();
 }
+template <class T, int NN> int launch_grad_p(const SsmArgs &a, hipStream_t st)
+{
+    if (a.P <= 32) return launch_grad<T, 32, NN>(a, st);
+    if (a.P <= 64) return launch_grad<T, 64, NN>(a, st);
+    return launch_grad<T, 128, NN>(a, st);
+}
 template <class T> int ssm_grad(const SsmArgs &a, hipStream_t st)
 {
-    constexpr int R = Parts<T>::raw;
-    const int most = a.P > a.N ? a.P : a.N;
-    if (most <= 32) return launch_grad<T, grad_block(R, 32), 32>(a, st);
-    if (most <= 64) return launch_grad<T, grad_block(R, 64), 64>(a, st);
-    return launch_grad<T, grad_block(R, 128), 128>(a, st);
+    if (a.N <= 32) return launch_grad_p<T, 32>(a, st);
+    if (a.N <= 64) return launch_grad_p<T, 64>(a, st);
+    return launch_grad_p<T, 128>(a, st);
 }
 
 }  // namespace semicrf_enc

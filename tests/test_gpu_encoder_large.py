@@ -68,6 +68,24 @@ def test_several_segments(P, N, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("P", [16, 40, 128])
+@pytest.mark.parametrize("N", [24, 64, 120])
+def test_every_pair_of_widths(P, N, dtype):
+    """Narrow heads with wide states and the reverse, each width padded by itself; once with two heads to a workgroup."""
+    for B, T, H, lengths in ((2, 70, 3, [70, 45]), (260, 5, 4, None)):
+        print("[case] ssm widths", B, P, N, dtype, flush=True)
+        d, h = make(B, T, H, P, 1, N, dtype, lengths, seed=47)
+        args = [h[k] for k in ("x", "b", "c", "dt", "rate", "skip", "dt_bias", "lengths", "state")]
+        y, last = forward(d)
+        ry, rlast, _ = plain.scan(*args)
+        assert far(y, ry) < TOL[dtype] and far(last, rlast) < F32_TOL
+        got, ref = backward(d), plain.scan_grad(*args, h["gy"], h["glast"])
+        for k, r in ref.items():
+            stored = k in ("grad_x", "grad_b", "grad_c", "grad_dt")
+            assert far(got[k], r) < (TOL[dtype] if stored else F32_TOL), k
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("B,H,P,G,N,W", [(300, 4, 72, 2, 40, 4), (520, 2, 64, 1, 128, 3)])
 def test_step_of_many_streams(B, H, P, G, N, W, dtype):
     print("[case] step", B, H, P, G, N, W, dtype, flush=True)
