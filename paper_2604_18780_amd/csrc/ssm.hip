@@ -255,7 +255,7 @@ struct StepArgs {
 // rather than in a launch before this one.  The ring holds the last W tokens at slot (position mod W), so the one slot that
 // is written is the one nobody reads.
 // Bound by the state, read and written once and past the caches (51 us through them); its loads are on their way before the
-// convolution starts: 192 streams of 16 heads of 64 x 128 take 41 us (206 MB, 5.1 TB/s).  One stream takes 5 us, a launch and
+// convolution starts: 192 streams of 16 heads of 64 x 128 take 39 us (206 MB, 5.3 TB/s).  One stream takes 5 us, a launch and
 // three loads that wait for one another.  Sixteen rows to a workgroup spread one stream over the chip; where there are
 // workgroups enough, 64 rows convolve B and C a quarter as often.
 template <class T, int R> __global__ __launch_bounds__(256) void k_ssm_step(StepArgs a)
