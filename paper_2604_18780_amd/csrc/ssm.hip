@@ -261,7 +261,8 @@ struct StepArgs {
 template <class T, int R> __global__ __launch_bounds__(256) void k_ssm_step(StepArgs a)
 {
     constexpr int ROWS = 16 * R;
-    __shared__ float sx[ROWS], sb[128], sc[128];
+    __shared__ __attribute__((aligned(16))) float sb[128], sc[128];  // read four at a time
+    __shared__ float sx[ROWS];
     const int tid = threadIdx.x, tiles = (a.P + ROWS - 1) / ROWS;
     const int tile = blockIdx.x % tiles, h = blockIdx.x / tiles % a.H, b = blockIdx.x / tiles / a.H;
     const int grp = h / (a.H / a.G), channels = a.H * a.P + 2 * a.G * a.N;

@@ -2,6 +2,8 @@
 #ifndef SEMICRF_SSM_BLOCK_H
 #define SEMICRF_SSM_BLOCK_H
 
+#include <stddef.h>
+
 #include "ssm_ops.h"
 
 namespace semicrf_enc {
@@ -188,7 +190,8 @@ __device__ __forceinline__ float pow2(double v) { return __builtin_amdgcn_exp2f(
 // Steps of a block of Q positions.  c is log2 of what is kept from the block's start to a position (REV: from its far end in
 // time, without the position's own step).  What is kept between two positions is 2^(c_i - c_j): between different sixteens it is
 // taken as query[i] * from[.][j], the two sides of the query's sixteen's first c, neither of which can overflow.
-template <int Q> struct Steps {
+// Four positions are read at once, of any element of an array of these: the size is a multiple of 16 bytes.
+template <int Q> struct alignas(16) Steps {
     double c[Q];
     float out[Q];               // 2^c
     float in[Q];                // what the state at the block's other end keeps of a position's term, times its scale
@@ -199,6 +202,11 @@ template <int Q> struct Steps {
     float from[Q / 16 - 1][Q];  // 2^(c of the first of sixteen k+1 - c_j) * key_j, for earlier j
     double total;               // log2 of what the block keeps
 };
+static_assert(sizeof(Steps<32>) % 16 == 0 && sizeof(Steps<64>) % 16 == 0, "four positions of any element are read as 16 bytes");
+static_assert(offsetof(Steps<32>, in) % 16 == 0 && offsetof(Steps<32>, key) % 16 == 0 && offsetof(Steps<32>, step) % 16 == 0 &&
+              offsetof(Steps<32>, from) % 16 == 0, "and of each member");
+static_assert(offsetof(Steps<64>, in) % 16 == 0 && offsetof(Steps<64>, key) % 16 == 0 && offsetof(Steps<64>, step) % 16 == 0 &&
+              offsetof(Steps<64>, from) % 16 == 0, "and of each member");
 
 // The value of another lane of the wave, by a fixed pattern; 0 where the pattern or the mask of rows of sixteen names none.
 template <int CTRL, int ROWS> __device__ __forceinline__ double other(double v)

@@ -26,7 +26,7 @@ template <class T, int Q, int DK, int PV, bool OUT> struct ScanShared {
     typedef Tile<T, Q, DK, PV * 4, false> TK;
     typedef Tile<T, Q, PV, PV * 4, false> TV;
     // one array, so that operands' places differ by constants
-    __bf16 pool[(OUT ? 2 : 1) * TK::ELEMS + TV::ELEMS + (OUT ? Scores<Q, Parts<T>::made>::ELEMS : 0)];
+    alignas(16) __bf16 pool[(OUT ? 2 : 1) * TK::ELEMS + TV::ELEMS + (OUT ? Scores<Q, Parts<T>::made>::ELEMS : 0)];
     Steps<Q> ss[AHEAD];
 };
 
