@@ -189,24 +189,26 @@ __device__ __forceinline__ float pow2(double v) { return __builtin_amdgcn_exp2f(
 
 // Steps of a block of Q positions.  c is log2 of what is kept from the block's start to a position (REV: from its far end in
 // time, without the position's own step).  What is kept between two positions is 2^(c_i - c_j): between different sixteens it is
-// taken as query[i] * from[.][j], the two sides of the query's sixteen's first c, neither of which can overflow.
+// taken as query[i] * from[j], the two sides of the query's sixteen's first c, neither of which can overflow.  A position's
+// term is scaled by its delta forwards, and by 1 backwards.
 // Four positions are read at once, of any element of an array of these: the size is a multiple of 16 bytes.
 template <int Q> struct alignas(16) Steps {
     double c[Q];
     float out[Q];               // 2^c
     float in[Q];                // what the state at the block's other end keeps of a position's term, times its scale
-    float key[Q];               // scale of a position's term
     float delta[Q];
     float step[Q];              // what is kept from the position before
-    float query[Q];             // 2^(c_i - c of the first of its sixteen)
-    float from[Q / 16 - 1][Q];  // 2^(c of the first of sixteen k+1 - c_j) * key_j, for earlier j
+    float query[Q - 16];        // of position 16 + i: 2^(c_i - c of the first of its sixteen)
+    float from[Q / 16 * (Q / 16 - 1) * 8];  // 2^(c of the first of sixteen k+1 - c_j), scaled, for the 16 k + 16 earlier j: a line for each k
     double total;               // log2 of what the block keeps
+    static constexpr __device__ __host__ int line(int k) { return 8 * k * (k + 1); }
 };
-static_assert(sizeof(Steps<32>) % 16 == 0 && sizeof(Steps<64>) % 16 == 0, "four positions of any element are read as 16 bytes");
-static_assert(offsetof(Steps<32>, in) % 16 == 0 && offsetof(Steps<32>, key) % 16 == 0 && offsetof(Steps<32>, step) % 16 == 0 &&
-              offsetof(Steps<32>, from) % 16 == 0, "and of each member");
-static_assert(offsetof(Steps<64>, in) % 16 == 0 && offsetof(Steps<64>, key) % 16 == 0 && offsetof(Steps<64>, step) % 16 == 0 &&
-              offsetof(Steps<64>, from) % 16 == 0, "and of each member");
+template <int Q> constexpr bool steps_aligned()
+{
+    return sizeof(Steps<Q>) % 16 == 0 && offsetof(Steps<Q>, in) % 16 == 0 && offsetof(Steps<Q>, delta) % 16 == 0 &&
+           offsetof(Steps<Q>, step) % 16 == 0 && offsetof(Steps<Q>, from) % 16 == 0;
+}
+static_assert(steps_aligned<32>() && steps_aligned<64>(), "four positions of any element are read as 16 bytes");
 
 // The value of another lane of the wave, by a fixed pattern; 0 where the pattern or the mask of rows of sixteen names none.
 template <int CTRL, int ROWS> __device__ __forceinline__ double other(double v)
@@ -224,7 +226,7 @@ __device__ __forceinline__ double of_lane(double v, int lane)
 }
 
 // One wave; lane = row (Q = 32: the upper half of the wave repeats nothing and writes nothing).
-template <int Q, bool REV> __device__ __forceinline__ void make_steps(Steps<Q> &s, float dt, float bias, float rate, bool scaled, int lane)
+template <int Q, bool REV> __device__ __forceinline__ void make_steps(Steps<Q> &s, float dt, float bias, float rate, int lane)
 {
     // a step beyond the sequence's end has delta = 0: nothing comes in and nothing is forgotten
     const float raw = dt + bias, delta = raw == -INFINITY ? 0.0f : softplus(raw);
@@ -239,7 +241,7 @@ template <int Q, bool REV> __device__ __forceinline__ void make_steps(Steps<Q> &
     if (Q == 64) c += other<0x143, 0xc>(c);  // lane 31, for rows 2 and 3
     const double total = of_lane(c, Q - 1);
     if (REV) c -= l;
-    const float key = scaled ? delta : 1.0f;
+    const float key = REV ? 1.0f : delta;
     double first = of_lane(c, 0);
     float from[Q / 16 - 1];
 #pragma unroll
@@ -252,12 +254,12 @@ template <int Q, bool REV> __device__ __forceinline__ void make_steps(Steps<Q> &
         s.c[lane] = c;
         s.out[lane] = pow2(c);
         s.in[lane] = pow2(total - c) * key;
-        s.key[lane] = key;
         s.delta[lane] = delta;
         s.step[lane] = pow2(step);
-        s.query[lane] = pow2(c - first);
+        if (lane >= 16) s.query[lane - 16] = pow2(c - first);
 #pragma unroll
-        for (int k = 0; k < Q / 16 - 1; ++k) s.from[k][lane] = from[k];
+        for (int k = 0; k < Q / 16 - 1; ++k)
+            if (lane < 16 * (k + 1)) s.from[Steps<Q>::line(k) + lane] = from[k];
         if (lane == 0) s.total = total;
     }
 }
@@ -265,23 +267,25 @@ template <int Q, bool REV> __device__ __forceinline__ void make_steps(Steps<Q> &
 // Weights of scores: sixteen queries `it`, sixteen keys `jt` <= it, as four keys of one query in a lane; 0 where the key lies
 // behind the query.  Where the two are the same sixteen, only the last of a lane's keys takes a power; the earlier ones
 // multiply what is kept on the way to it.
-template <int Q> __device__ __forceinline__ f4 weights(const Steps<Q> &s, int it, int jt, int i16, int g)
+template <int Q, bool REV> __device__ __forceinline__ f4 weights(const Steps<Q> &s, int it, int jt, int i16, int g)
 {
-    if (jt < it) return *(const f4 *)(s.from[it - 1] + 16 * jt + 4 * g) * s.query[16 * it + i16];
-    const f4 key = *(const f4 *)(s.key + 16 * it + 4 * g), step = *(const f4 *)(s.step + 16 * it + 4 * g);
+    if (jt < it) return *(const f4 *)(s.from + Steps<Q>::line(it - 1) + 16 * jt + 4 * g) * s.query[16 * (it - 1) + i16];
+    const f4 step = *(const f4 *)(s.step + 16 * it + 4 * g);
     const float last = fminf((float)(s.c[16 * it + i16] - s.c[16 * it + 4 * g + 3]), 0.0f);
     f4 e;
     e[3] = i16 >= 4 * g + 3 ? __builtin_amdgcn_exp2f(last) : 0.0f;
 #pragma unroll
     for (int r = 2; r >= 0; --r) e[r] = i16 == 4 * g + r ? 1.0f : e[r + 1] * step[r + 1];
-    return e * key;
+    return REV ? e : e * *(const f4 *)(s.delta + 16 * it + 4 * g);
 }
 
 // Where scores are handed from the wave that makes them to those that multiply with them: operands of queries 16 it.., keys
-// 32 ks.., ks <= it / 2; each is two tiles of sixteen keys, of which the second may lie behind the queries (zeros).
-template <int Q, int MADE> struct Scores {
-    static constexpr int IT = Q / 16, TILES = IT * (IT + 1) / 2, OPS = IT == 4 ? 6 : 2, ELEMS = OPS * MADE * 64 * 8;
-    static constexpr __device__ __host__ int op(int it, int ks) { return it < 2 ? it : 2 * it - 2 + ks; }
+// 32 ks.., ks <= it / 2; each is two tiles of sixteen keys, of which the second, where it lies behind the queries (keys from
+// 16 it on, it even), is not stored but zeros.
+template <int Q> struct Scores {
+    static constexpr int IT = Q / 16, TILES = IT * (IT + 1) / 2, ELEMS = TILES * HELD * 64 * 4;
+    static constexpr __device__ __host__ bool half(int it, int ks) { return 2 * ks == it; }
+    static constexpr __device__ __host__ int first(int it, int ks) { return (it * (it + 1) / 2 + 2 * ks) * HELD * 64 * 4; }
     // tile k of the block, and the wave of NW that makes it: with four waves three, three, two and two, sixteen keys each
     static constexpr __device__ int query(int k) { return IT == 2 ? (k > 0) : k == 0 ? 0 : k == 1 || k == 3 ? 1 : k == 4 || k == 6 || k == 9 ? 2 : 3; }
     static constexpr __device__ int keys(int k) { return IT == 2 ? k / 2 : k < 3 || k == 9 ? 0 : k < 6 ? 1 : k < 8 ? 2 : 3; }
@@ -289,23 +293,23 @@ template <int Q, int MADE> struct Scores {
     static __device__ __forceinline__ void put(__bf16 *sm, int it, int jt, f4 v, int lane)
     {
         float x[4] = {v[0], v[1], v[2], v[3]};
-        uint32_t p[MADE][2];
-        split_pairs<MADE, 2>(x, p);
+        uint32_t p[HELD][2];
+        split_pairs<HELD, 2>(x, p);
+        const int wide = half(it, jt / 2) ? 4 : 8;
 #pragma unroll
-        for (int k = 0; k < MADE; ++k)
-            *(u2 *)(sm + ((op(it, jt / 2) * MADE + k) * 64 + lane) * 8 + 4 * (jt & 1)) = (u2){p[k][0], p[k][1]};
+        for (int k = 0; k < HELD; ++k) *(u2 *)(sm + first(it, jt / 2) + (k * 64 + lane) * wide + 4 * (jt & 1)) = (u2){p[k][0], p[k][1]};
     }
-    // zeros where an operand's second tile lies behind its queries; once, by the whole workgroup
-    static __device__ __forceinline__ void clear(__bf16 *sm, int tid, int nt)
+    // acc + v * the scores of queries 16 it.. and keys 32 ks..
+    template <int n> static __device__ __forceinline__ f4 product(f4 acc, const Op<n> &v, const __bf16 *sm, int it, int ks, int lane)
     {
-        for (int k = tid; k < ELEMS / 8; k += nt) *(u4 *)(sm + 8 * k) = (u4)0u;
-    }
-    static __device__ __forceinline__ Op<MADE> get(const __bf16 *sm, int m, int lane)
-    {
-        Op<MADE> o;
+        const __bf16 *p = sm + first(it, ks) + lane * (half(it, ks) ? 4 : 8);
+        Op<HELD> s;
 #pragma unroll
-        for (int k = 0; k < MADE; ++k) o.p[k] = *(const bf8 *)(sm + ((m * MADE + k) * 64 + lane) * 8);
-        return o;
+        for (int k = 0; k < HELD; ++k) {
+            if (half(it, ks)) s.p[k] = __builtin_shufflevector(*(const bf4 *)(p + k * 64 * 4), (bf4)(__bf16)0.0f, 0, 1, 2, 3, 4, 5, 6, 7);
+            else s.p[k] = *(const bf8 *)(p + k * 64 * 8);
+        }
+        return mma(acc, v, s);
     }
 };
 

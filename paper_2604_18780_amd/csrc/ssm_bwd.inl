@@ -117,16 +117,16 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
 {
     constexpr int Q = GRAD_BLOCK, MOST = PP > NN ? PP : NN, NT = MOST * 4, NW = MOST / 16, IT = Q / 16, QS = Q / 32;
     constexpr int KTP = PP / 16, KTN = NN / 16, KSP = PP / 32, KSN = NN / 32;
-    constexpr int RAW = Parts<T>::raw, MADE = Parts<T>::made, HELD = 3, E = (int)sizeof(T);
+    constexpr int RAW = Parts<T>::raw, E = (int)sizeof(T);
     typedef Tile<T, Q, PP, NT, false> TP;
     typedef Tile<T, Q, NN, NT, false> TN;
-    typedef Scores<Q, MADE> SC;
+    typedef Scores<Q> SC;
     constexpr int OWN = (SC::TILES + NW - 1) / NW;  // tiles of scores a wave makes at most
     constexpr int TURNS = (IT + NW - 1) / NW;       // sixteens of positions whose sums a wave makes
     // one array, so that operands' places differ by constants
     __shared__ __attribute__((aligned(16))) __bf16 pool[2 * TP::ELEMS + 2 * TN::ELEMS + SC::ELEMS];
     __bf16 *const sx = pool, *const sy = sx + TP::ELEMS, *const sb = sy + TP::ELEMS, *const sc = sb + TN::ELEMS, *const sm = sc + TN::ELEMS;
-    __shared__ __attribute__((aligned(16))) Steps<Q> ss[2][HB];
+    __shared__ Steps<Q> ss[2];  // of this head and the next
     __shared__ float rp[NW][Q];             // by wave: its columns' part of rint
     __shared__ float ends[SC::TILES][16];   // sums of a tile of W by its later positions (on the diagonal: dlin), ..
     __shared__ float starts[SC::TILES][16]; // .. and by its earlier ones
@@ -168,24 +168,22 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
             }
         }
     }
-    // Steps are made a block ahead, by the last wave, which has the fewest scores to make; dt comes another block ahead.
-    Dt<T> dt[HB];
+    // Steps are made a head ahead, by the last wave, which has the fewest scores to make; dt comes another head ahead.
+    Dt<T> dt;
+    const bool two = HB > 1 && at.nh > 1;  // heads in turn
     auto fetch_dt = [&](int n, int k) {
-        dt[k].fetch(src.dt + (int64_t)Q * n * src.dt_bytes + (k < at.nh ? k * E : 0), src.dt_bytes, lane % Q, n < at.nblk ? at.L - at.t0 - Q * n : 0);
+        dt.fetch(src.dt + (int64_t)Q * n * src.dt_bytes + k * E, src.dt_bytes, lane % Q, n < at.nblk ? at.L - at.t0 - Q * n : 0);
     };
     if (at.nblk) {
         rbt.fetch(rows_at(src.b, at.L - at.t0, Q, src.b_bytes), 0);
         rct.fetch(rows_at(src.c, at.L - at.t0, Q, src.c_bytes), 0);
         rx.fetch(rows_at(src.x, at.L - at.t0, Q, src.x_bytes), 0);
         ry.fetch(rows_at(src.y, at.L - at.t0, Q, src.y_bytes), 0);
-        SC::clear(sm, tid, NT);
-#pragma unroll
-        for (int k = 0; k < HB; ++k) {
-            fetch_dt(0, k);
-            if (w == k % NW) make_steps<Q, false>(ss[0][k], dt[k].value(), bias[k], rate[k], true, lane);
-            fetch_dt(1, k);
-        }
+        fetch_dt(0, 0);
+        if (w == 0) make_steps<Q, false>(ss[0], dt.value(), bias[0], rate[0], lane);
+        fetch_dt(two ? 0 : 1, two ? 1 : 0);
     }
+    int turn = 0;  // counts heads
     const SharedOut<T> out(a, a.gc, a.gc_row, a.partc, a.chunks, at);
     for (int n = 0; n < at.nblk; ++n) {
         const int base = at.t0 + Q * n;
@@ -230,7 +228,7 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
                     ++own;
                 }
             }
-            const Steps<Q> &s = ss[n & 1][k];
+            const Steps<Q> &s = ss[turn & 1];
             int own = 0;
 #pragma unroll
             for (int m = 0; m < SC::TILES; ++m) {
@@ -240,7 +238,7 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
 #pragma unroll
                 for (int ks = 0; ks < KSP; ++ks)
                     p = mma_inputs(p, TP::by_row(sx, lp, jt, ks), TP::by_row(sy, lp, it, ks));
-                p *= weights(s, it, jt, i16, g);
+                p *= weights<Q, false>(s, it, jt, i16, g);
                 SC::put(sm, it, jt, p, lane);
 #pragma unroll
                 for (int o = 1; o < OWN; ++o)
@@ -268,8 +266,12 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
                     }
                 }
             }
-            if (w == NW - 1) make_steps<Q, false>(ss[(n + 1) & 1][k], dt[k].value(), bias[k], rate[k], true, lane);
-            fetch_dt(n + 2, k);
+            if (w == NW - 1) {
+                const int next = k + 1 < HB ? k + 1 : 0;
+                const bool same = two && k == 0;
+                make_steps<Q, false>(ss[(turn + 1) & 1], dt.value(), same ? bias[next] : bias[0], same ? rate[next] : rate[0], lane);
+            }
+            fetch_dt(two ? n + 1 : n + 2, two ? k : 0);
             if (own_n) {
                 // what the state at the block's start gives
                 f4 F[IT];
@@ -308,7 +310,7 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
             for (int it = 0; it < IT; ++it)
 #pragma unroll
                 for (int ks = 0; ks <= it / 2; ++ks)
-                    if (own_n) O[it] = mma(O[it], v[ks], SC::get(sm, SC::op(it, ks), lane));
+                    if (own_n) O[it] = SC::product(O[it], v[ks], sm, it, ks, lane);
             // sums over waves and tiles: each wave those of its sixteens, lane = position
             const size_t line = (size_t)(at.b * a.H + at.h0 + k) * a.T;
 #pragma unroll
@@ -334,6 +336,7 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
                 put_line<Q>(a.rint + line, base, at.t1, K < IT && g == 0 ? at16 : -1, ri);
                 put_line<Q>(a.dlin + line, base, at.t1, K < IT && g == 0 ? at16 : -1, dl);
             }
+            ++turn;
         }
 #pragma unroll
         for (int it = 0; it < IT; ++it) out.template put<Q>(base, i16, 16 * it, 16 * w + 4 * g, a.N, at.t1, O[it]);
@@ -346,25 +349,24 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
 //   du_j = sum_{i>=j} e^{c_i-c_j} (B_j . C_i) dy_i     queries B, keys C, values dy; state G [N x P]     dx = delta du + skip dy
 //   dB_j = sum_h delta_j sum_{i>=j} e^{c_i-c_j} (x_j . dy_i) C_i     queries x, keys dy, values C; state G^T [P x N]
 // Rows run backwards in time.  A wave holds sixteen columns p of G; its parts, which the product with B needs anyway, go through
-// LDS, from where they are read transposed for the product with x.  Only float32 at a width of 128 has no room for that (98 KB):
-// there a wave holds sixteen columns n of the transpose as well, at twice the products for the updates.
+// LDS, from where they are read transposed for the product with x.  Only float32 and float16 at 128 x 128 have no room for that
+// (98 KB): there a wave holds sixteen columns n of the transpose as well, at twice the products for the updates.
 template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN ? PP : NN) * 4, waves_for(Parts<T>::raw, PP > NN ? PP : NN)) void k_ssm_grad_xb(SsmArgs a)
 {
     constexpr int Q = GRAD_BLOCK, MOST = PP > NN ? PP : NN, NT = MOST * 4, NW = MOST / 16, IT = Q / 16, QS = Q / 32;
     constexpr int KTP = PP / 16, KTN = NN / 16, KSP = PP / 32, KSN = NN / 32;
-    constexpr int RAW = Parts<T>::raw, MADE = Parts<T>::made, HELD = 3, E = (int)sizeof(T);
+    constexpr int RAW = Parts<T>::raw, E = (int)sizeof(T);
     typedef Tile<T, Q, PP, NT, true> TP;
     typedef Tile<T, Q, NN, NT, true> TN;
-    typedef Scores<Q, HELD> SU;  // for the gradient of u, which goes into those of the steps as well
-    typedef Scores<Q, MADE> SC;
+    typedef Scores<Q> SC;
     constexpr int OWN = (SC::TILES + NW - 1) / NW, TURNS = (IT + NW - 1) / NW;
-    constexpr bool TWICE = RAW == 3 && PP == 128 && NN == 128;
+    constexpr bool TWICE = RAW >= 2 && PP == 128 && NN == 128;
     // one array, so that operands' places differ by constants
-    __shared__ __attribute__((aligned(16))) __bf16 pool[2 * TP::ELEMS + 2 * TN::ELEMS + SU::ELEMS + SC::ELEMS + (TWICE ? 0 : MADE * PP * NN)];
+    __shared__ __attribute__((aligned(16))) __bf16 pool[2 * TP::ELEMS + 2 * TN::ELEMS + 2 * SC::ELEMS + (TWICE ? 0 : HELD * PP * NN)];
     __bf16 *const sx = pool, *const sy = sx + TP::ELEMS, *const sb = sy + TP::ELEMS, *const sc = sb + TN::ELEMS, *const su = sc + TN::ELEMS,
-        *const sm = su + SU::ELEMS, *const sg = sm + SC::ELEMS;  // sg: G [p][n]
-    __shared__ __attribute__((aligned(16))) Steps<Q> ss[2][HB];
-    __shared__ __attribute__((aligned(16))) float qp[2][NW][Q], xp[2][NW][Q];  // by wave: its columns' part of qint and x . du; of this head and the one before
+        *const sm = su + SC::ELEMS, *const sg = sm + SC::ELEMS;  // sg: G [p][n]
+    __shared__ Steps<Q> ss[2];  // of this head and the next
+    __shared__ __attribute__((aligned(16))) float qp[2][NW][Q], xp[NW][Q];  // by wave: its columns' part of qint (of this head and the one before) and of x . du
 
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, i16 = lane & 15;
     const Place<T> at(a, HB, Q, a.chunks);
@@ -413,10 +415,10 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
             }
         }
     }
-    Dt<T> dt[HB];
+    Dt<T> dt;
+    const bool two = HB > 1 && at.nh > 1;  // heads in turn
     auto fetch_dt = [&](int n, int k) {
-        dt[k].fetch(src.dt + (k < at.nh ? k * E : 0) - (int64_t)Q * n * src.dt_bytes, src.dt_bytes, Q - 1 - lane % Q,
-                    n < at.nblk ? at.L - base_of(n) : 0);
+        dt.fetch(src.dt + k * E - (int64_t)Q * n * src.dt_bytes, src.dt_bytes, Q - 1 - lane % Q, n < at.nblk ? at.L - base_of(n) : 0);
     };
     if (at.nblk) {
         const int left = at.L - base_of(0);
@@ -424,30 +426,25 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
         rct.fetch(rows_at(src.c, left, Q, src.c_bytes), 0);
         rx.fetch(rows_at(src.x, left, Q, src.x_bytes), 0);
         ry.fetch(rows_at(src.y, left, Q, src.y_bytes), 0);
-        SU::clear(su, tid, NT);
-        SC::clear(sm, tid, NT);
-#pragma unroll
-        for (int k = 0; k < HB; ++k) {
-            fetch_dt(0, k);
-            if (w == k % NW) make_steps<Q, true>(ss[0][k], dt[k].value(), bias[k], rate[k], false, lane);
-            fetch_dt(1, k);
-        }
+        fetch_dt(0, 0);
+        if (w == 0) make_steps<Q, true>(ss[0], dt.value(), bias[0], rate[0], lane);
+        fetch_dt(two ? 0 : 1, two ? 1 : 0);
     }
     const SharedOut<T> out(a, a.gb, a.gb_row, a.partb, a.chunks, at);
     const int gx_bytes = (int)a.gx_row * E;
     char *gxs = (char *)a.gx + (at.rb + (at.nblk ? base_of(0) : at.t0)) * gx_bytes + at.h0 * a.P * E;
     const uint32_t gx_off = 16 * w + 4 * g < a.P ? (uint32_t)((15 - i16) * gx_bytes + (16 * w + 4 * g) * E) : OUTSIDE;
-    // The sums of a head over the waves are made while the next one is worked on: `turn` counts heads.
+    // The sums of a head over the waves are made while the next one is worked on, until its second barrier; `turn` counts heads.
     int turn = 0;
     auto join = [&](int n, int k, bool any) {
         const size_t line = (size_t)(at.b * a.H + at.h0 + k) * a.T;
-        const int p = (turn & 1) ^ 1, base = base_of(n);
+        const int base = base_of(n);
 #pragma unroll
         for (int x = 0; x < TURNS; ++x) {
             const int K = w + NW * x, at16 = 16 * K + i16;
             float q = 0.0f, s = 0.0f;
             if (K < IT)
-                for (int y = 0; y < KTP; ++y) q += qp[p][y][at16], s += xp[p][y][at16];
+                for (int y = 0; y < KTP; ++y) q += qp[(turn & 1) ^ 1][y][at16], s += xp[y][at16];
             put_line<Q>(a.qint + line, base, at.t1, any && K < IT && g == 0 ? Q - 1 - at16 : -1, q);
             put_line<Q>(a.xdu + line, base, at.t1, any && K < IT && g == 0 ? Q - 1 - at16 : -1, s);
         }
@@ -471,7 +468,7 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
                 for (int ks = 0; ks < KSN; ++ks) {
                     st[ks] = split<HELD>(__builtin_shufflevector(S[k][2 * ks], S[k][2 * ks + 1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-                    for (int part = 0; part < (TWICE ? 0 : MADE); ++part) {
+                    for (int part = 0; part < (TWICE ? 0 : HELD); ++part) {
                         const u4 v = __builtin_bit_cast(u4, st[ks].p[part]);
                         __bf16 *to = sg + part * PP * NN + 16 * wp * NN + ks / 2 * 64;
                         *(u2 *)(to + ln.row[NN >= 64 ? ks % 2 * 2 : 0]) = (u2){v[0], v[1]};
@@ -512,7 +509,7 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
                     ++own;
                 }
             }
-            const Steps<Q> &s = ss[n & 1][k];
+            const Steps<Q> &s = ss[turn & 1];
             f4 U[IT];
 #pragma unroll
             for (int it = 0; it < IT; ++it) U[it] = (f4)0.0f;
@@ -539,12 +536,16 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
                 for (int o = 1; o < OWN; ++o)
                     if (o == own) d = D[o];
                 ++own;
-                const f4 f = weights(s, it, jt, i16, g);
-                SU::put(su, it, jt, d * f, lane);
+                const f4 f = weights<Q, true>(s, it, jt, i16, g);
+                SC::put(su, it, jt, d * f, lane);
                 SC::put(sm, it, jt, p * (f * s.delta[16 * it + i16]), lane);
             }
-            if (w == NW - 1) make_steps<Q, true>(ss[(n + 1) & 1][k], dt[k].value(), bias[k], rate[k], false, lane);
-            fetch_dt(n + 2, k);
+            if (w == NW - 1) {
+                const int next = k + 1 < HB ? k + 1 : 0;
+                const bool same = two && k == 0;
+                make_steps<Q, true>(ss[(turn + 1) & 1], dt.value(), same ? bias[next] : bias[0], same ? rate[next] : rate[0], lane);
+            }
+            fetch_dt(two ? n + 1 : n + 2, two ? k : 0);
             // what the state behind the block gives to the gradient of B ..
             if (own_n) {
                 f4 F[IT];
@@ -552,9 +553,9 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
                 for (int it = 0; it < IT; ++it) F[it] = (f4)0.0f;
 #pragma unroll
                 for (int ks = 0; ks < KSP; ++ks) {
-                    Op<MADE> gt;
-                    if constexpr (TWICE) gt = split<MADE>(__builtin_shufflevector(R[k][2 * ks], R[k][2 * ks + 1], 0, 1, 2, 3, 4, 5, 6, 7));
-                    else gt = TN::template transposed<MADE>(sg, ln.own, 32 * ks * NN, PP * NN);
+                    Op<HELD> gt;
+                    if constexpr (TWICE) gt = split<HELD>(__builtin_shufflevector(R[k][2 * ks], R[k][2 * ks + 1], 0, 1, 2, 3, 4, 5, 6, 7));
+                    else gt = TN::template transposed<HELD>(sg, ln.own, 32 * ks * NN, PP * NN);
 #pragma unroll
                     for (int it = 0; it < IT; ++it) F[it] = mma(F[it], gt, TP::by_row(sx, lp, it, ks));
                 }
@@ -588,7 +589,7 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
 #pragma unroll
                     for (int kt = 0; kt < KTN; ++kt) S[k][kt] = mma(S[k][kt], TN::by_col(sc, ln, ks, kt), u);
                     if constexpr (TWICE) {
-                        const Op<MADE> v = split<MADE>(values(vc[ks]) * in);
+                        const Op<HELD> v = split<HELD>(values(vc[ks]) * in);
 #pragma unroll
                         for (int kt = 0; kt < KTP; ++kt) R[k][kt] = mma(ks ? R[k][kt] : R[k][kt] * keep, TP::by_col(sy, lp, ks, kt), v);
                     }
@@ -599,16 +600,16 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
 #pragma unroll
                 for (int it = 0; it < IT; ++it)
 #pragma unroll
-                    for (int ks = 0; ks <= it / 2; ++ks) O[it] = mma(O[it], vc[ks], SC::get(sm, SC::op(it, ks), lane));
+                    for (int ks = 0; ks <= it / 2; ++ks) O[it] = SC::product(O[it], vc[ks], sm, it, ks, lane);
             }
 #pragma unroll
             for (int it = 0; it < IT; ++it) {
                 const int r = 16 * it + i16;
 #pragma unroll
-                for (int ks = 0; ks <= it / 2; ++ks) U[it] = mma(U[it], vy[ks], SU::get(su, SU::op(it, ks), lane));
+                for (int ks = 0; ks <= it / 2; ++ks) U[it] = SC::product(U[it], vy[ks], su, it, ks, lane);
                 const f4 e = U[it] * xv[it], o = U[it] * s.delta[r] + yv[it] * skip[k];
                 const float sum = sum_rows(e[0] + e[1] + e[2] + e[3]);
-                if (g == 0) xp[turn & 1][w][r] = sum;
+                if (g == 0) xp[w][r] = sum;
                 store_four<T>(rows_at(gxs, at.t1 - base, Q, gx_bytes), gx_off, 16 * (IT - 1 - it) * gx_bytes + k * a.P * E, o);
             }
             ++turn;

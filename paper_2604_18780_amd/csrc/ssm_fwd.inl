@@ -26,7 +26,7 @@ template <class T, int Q, int DK, int PV, bool OUT> struct ScanShared {
     typedef Tile<T, Q, DK, PV * 4, false> TK;
     typedef Tile<T, Q, PV, PV * 4, false> TV;
     // one array, so that operands' places differ by constants
-    alignas(16) __bf16 pool[(OUT ? 2 : 1) * TK::ELEMS + TV::ELEMS + (OUT ? Scores<Q, Parts<T>::made>::ELEMS : 0)];
+    alignas(16) __bf16 pool[(OUT ? 2 : 1) * TK::ELEMS + TV::ELEMS + (OUT ? Scores<Q>::ELEMS : 0)];
     Steps<Q> ss[AHEAD];
 };
 
@@ -35,13 +35,13 @@ __device__ __forceinline__ void scan_segment(const SsmArgs &a, unsigned block, S
 {
     constexpr int NT = PV * 4, NW = PV / 16, KT = DK / 16, KS = DK / 32, IT = Q / 16, QS = Q / 32;
     constexpr int AHEAD = ScanShared<T, Q, DK, PV, OUT>::AHEAD;
-    constexpr int RAW = Parts<T>::raw, MADE = Parts<T>::made, HELD = 3;
+    constexpr int RAW = Parts<T>::raw;
     // queries are kept from the scores to the output, except where they would take 96 registers (float32, 128 states: 343 us so, 305
     // read again; bfloat16 138 us kept, 154 read again; 16 x 4000 positions of 8 heads of 64)
     constexpr bool HOLD = IT * KS * RAW <= 16;
     typedef Tile<T, Q, DK, NT, REV> TK;
     typedef Tile<T, Q, PV, NT, REV> TV;
-    typedef Scores<Q, MADE> SC;
+    typedef Scores<Q> SC;
     __bf16 *const sk = sh.pool, *const sv = sk + TK::ELEMS, *const sq = sv + TV::ELEMS, *const sm = sq + (OUT ? TK::ELEMS : 0);
     Steps<Q> *const ss = sh.ss;
 
@@ -110,15 +110,12 @@ __device__ __forceinline__ void scan_segment(const SsmArgs &a, unsigned block, S
 #pragma unroll
     for (int r = 0; r < 4; ++r) skips[r] = 4 * g + r == i16 ? skip : 0.0f;
     fetch_dt(w);
-    if (nblk) {
-        fetch(0);
-        if constexpr (OUT) SC::clear(sm, tid, NT);
-    }
+    if (nblk) fetch(0);
     for (int n = 0; n < nblk; ++n) {
         const int base = at(n);
         const Steps<Q> &s = ss[n % AHEAD];
         if (n % AHEAD == 0 && w < AHEAD) {
-            make_steps<Q, REV>(ss[w], dt_next.value(), bias, rate, !REV, lane);
+            make_steps<Q, REV>(ss[w], dt_next.value(), bias, rate, lane);
             fetch_dt(n + AHEAD + w);
         }
         if constexpr (OUT) rq.put(sq, pk, tid);
@@ -146,7 +143,7 @@ __device__ __forceinline__ void scan_segment(const SsmArgs &a, unsigned block, S
                 f4 m = (f4)0.0f;
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) m = mma_inputs(m, TK::by_row(sk, lk, jt, ks), q(it, ks));
-                m *= weights(s, it, jt, i16, g);
+                m *= weights<Q, REV>(s, it, jt, i16, g);
                 if (it == jt) m += skips;
                 SC::put(sm, it, jt, m, lane);
             }
@@ -155,7 +152,7 @@ __device__ __forceinline__ void scan_segment(const SsmArgs &a, unsigned block, S
             for (int it = 0; it < IT; ++it) O[it] = (f4)0.0f;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                const Op<MADE> st = split<MADE>(__builtin_shufflevector(S[2 * ks], S[2 * ks + 1], 0, 1, 2, 3, 4, 5, 6, 7));
+                const Op<HELD> st = split<HELD>(__builtin_shufflevector(S[2 * ks], S[2 * ks + 1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
                 for (int it = 0; it < IT; ++it) O[it] = mma(O[it], st, q(it, ks));
             }
@@ -184,7 +181,7 @@ __device__ __forceinline__ void scan_segment(const SsmArgs &a, unsigned block, S
 #pragma unroll
             for (int it = 0; it < IT; ++it)
 #pragma unroll
-                for (int ks = 0; ks <= it / 2; ++ks) O[it] = mma(O[it], v[ks], SC::get(sm, SC::op(it, ks), lane));
+                for (int ks = 0; ks <= it / 2; ++ks) O[it] = SC::product(O[it], v[ks], sm, it, ks, lane);
             // a lane holds channels 16 w + 4g .. +3 of positions i16, 16 + i16, ..
             const __amdgpu_buffer_rsrc_t rows = rows_at(ys, t1 - base, Q, y_bytes);
             ys += (int64_t)Q * y_bytes;

@@ -2,9 +2,7 @@
 //
 // The matrix cores multiply bfloat16.  Operands that are wider are split into bfloat16 parts whose sum holds 8, 16 or 24
 // bits, and the products of parts that matter are added up in 32 bits: bfloat16 inputs are exact in one part, float16 in two,
-// float32 takes three.  What is computed on the way takes two or three, by what it goes into: two leave 2^-17 of a term, which
-// is less than the rounding of an output stored in two bytes; states and the gradients of the steps, whose sums are returned
-// in 32 bits, take three (2^-25).
+// float32 takes three, and so does what is computed on the way (states, scores), whatever the type: 24 bits, 2^-25 of a term.
 //
 // With g = lane / 16, a lane holds rows 4g..4g+3 of one column of a 16 x 16 result, and eight inner indexes of one row (or column)
 // of an operand: any eight, as long as both operands hold the same.  They are 4g..4g+3 of each of two tiles of 16, so that two
@@ -20,10 +18,11 @@ typedef __bf16 bf4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
 typedef short s4 __attribute__((ext_vector_type(4)));
 
-template <class T> struct Parts;  // of an input, and of what goes only into outputs of this type
-template <> struct Parts<__bf16> { static constexpr int raw = 1, made = 2; };
-template <> struct Parts<_Float16> { static constexpr int raw = 2, made = 2; };
-template <> struct Parts<float> { static constexpr int raw = 3, made = 3; };
+template <class T> struct Parts;  // of an input
+template <> struct Parts<__bf16> { static constexpr int raw = 1; };
+template <> struct Parts<_Float16> { static constexpr int raw = 2; };
+template <> struct Parts<float> { static constexpr int raw = 3; };
+constexpr int HELD = 3;           // of what is computed on the way
 
 template <int n> struct Op { bf8 p[n]; };
 
