@@ -464,7 +464,7 @@ int semicrf_conv_bwd(const void *u, int64_t u_row, const float *weight, const fl
  * Selective state space scan.  For each head h of H (P channels, a P x N state) with delta = softplus(dt + dt_bias):
  *     H_t = exp(delta_t rate) H_{t-1} + delta_t x_t B_t^T          y_t = H_t C_t + skip x_t
  *   x, y [B,T,H*P], b, c [B,T,G*N], dt [B,T,H] activations; each of G groups of H/G heads shares B_t and C_t
- *   rate, skip (or NULL: 0), dt_bias (or NULL: 0) [H] float; rate < 0 is what forgets
+ *   rate, skip (or NULL: 0), dt_bias (or NULL: 0) [H] float; rate < 0 forgets, rate > 0 grows (as far as float32 reaches)
  *   state, state_out [B,H,P,N] float or NULL: the state before the first and after the last valid token (NULL: zeros / not
  *          wanted); may be the same array, so a prompt can be taken in pieces
  * P and N are multiples of 8 up to 128.  Workspace: semicrf_ssm_workspace_bytes, want_grad = 0 for semicrf_ssm_fwd (may be 0

@@ -189,7 +189,7 @@ __device__ __forceinline__ float pow2(double v) { return __builtin_amdgcn_exp2f(
 
 // Steps of a block of Q positions.  c is log2 of what is kept from the block's start to a position (REV: from its far end in
 // time, without the position's own step).  What is kept between two positions is 2^(c_i - c_j): between different sixteens it is
-// taken as query[i] * from[j], the two sides of the query's sixteen's first c, neither of which can overflow.  A position's
+// taken as query[i] * from[j], the two sides of the query's sixteen's first c, neither of which overflows where their product does not.  A position's
 // term is scaled by its delta forwards, and by 1 backwards.
 // Four positions are read at once, of any element of an array of these: the size is a multiple of 16 bytes.
 template <int Q> struct alignas(16) Steps {
@@ -271,7 +271,7 @@ template <int Q, bool REV> __device__ __forceinline__ f4 weights(const Steps<Q> 
 {
     if (jt < it) return *(const f4 *)(s.from + Steps<Q>::line(it - 1) + 16 * jt + 4 * g) * s.query[16 * (it - 1) + i16];
     const f4 step = *(const f4 *)(s.step + 16 * it + 4 * g);
-    const float last = fminf((float)(s.c[16 * it + i16] - s.c[16 * it + 4 * g + 3]), 0.0f);
+    const float last = (float)(s.c[16 * it + i16] - s.c[16 * it + 4 * g + 3]);
     f4 e;
     e[3] = i16 >= 4 * g + 3 ? __builtin_amdgcn_exp2f(last) : 0.0f;
 #pragma unroll
