@@ -98,8 +98,9 @@ constexpr int MOST_BLOCKS = 32;  // of a segment of 1024
 
 template <class T> __global__ __launch_bounds__(64) void k_ssm_steps(SsmArgs a)
 {
-    __shared__ double over[MOST_BLOCKS], qs[MOST_BLOCKS], rs[MOST_BLOCKS];
-    __shared__ float ks[MOST_BLOCKS], q2[MOST_BLOCKS], r2[MOST_BLOCKS], var[MOST_BLOCKS];
+    // variances in 64 bits: squares of float32 values need not fit in 32
+    __shared__ double over[MOST_BLOCKS], qs[MOST_BLOCKS], rs[MOST_BLOCKS], q2[MOST_BLOCKS], r2[MOST_BLOCKS], var[MOST_BLOCKS];
+    __shared__ float ks[MOST_BLOCKS];
     constexpr int Q = GRAD_BLOCK;
     const int lane = threadIdx.x, r = lane & (Q - 1);
     const int seg = blockIdx.x % a.nseg, bh = blockIdx.x / a.nseg, h = bh % a.H, b = bh / a.H;
@@ -116,7 +117,7 @@ template <class T> __global__ __launch_bounds__(64) void k_ssm_steps(SsmArgs a)
         const size_t at = (size_t)bh * a.T + t;
         double q = in ? (double)a.qint[at] : 0.0, ri = in ? (double)a.rint[at] : 0.0;
         float kept = in ? softplus((float)dts[t * a.dt_row] + bias) : 0.0f;
-        float qq = (float)(q * q), rr = (float)(ri * ri);
+        double qq = q * q, rr = ri * ri;
         for (int d = 1; d < Q; d *= 2) {
             q += __shfl_xor(q, d), ri += __shfl_xor(ri, d), kept += __shfl_xor(kept, d);
             qq += __shfl_xor(qq, d), rr += __shfl_xor(rr, d);
@@ -136,8 +137,8 @@ template <class T> __global__ __launch_bounds__(64) void k_ssm_steps(SsmArgs a)
     __syncthreads();
     {
         double across = cross[1];
-        float spread = (float)(cross[1] * cross[1]);  // the walk's variance
-        int first = nblk;                             // its blocks: up to here
+        double spread = cross[1] * cross[1];  // the walk's variance
+        int first = nblk;                     // its blocks: up to here
         for (int n = nblk - 1; n >= 0; --n) {
             const double qi = qs[n], ri = rs[n];
             const bool gone = ks[n] * rate * 1.44269504f < -30.0f;
@@ -146,14 +147,14 @@ template <class T> __global__ __launch_bounds__(64) void k_ssm_steps(SsmArgs a)
             if (lane == 0) over[n] = across, var[n] = spread;
             if (gone || n == 0) {
                 const double off = gone ? across : across + ri - cross[0];
-                const float all = gone ? spread : spread + r2[n] + (float)(cross[0] * cross[0]);
+                const double all = gone ? spread : spread + r2[n] + cross[0] * cross[0];
                 __syncthreads();
-                if (lane < first - n && all > 0.0f) over[n + lane] -= off * (double)(var[n + lane] / all);
+                if (lane < first - n && all > 0.0) over[n + lane] -= off * (var[n + lane] / all);
                 __syncthreads();
                 if (gone && lane == 0) over[n] = 0.0;
                 first = n;
                 across = 0.0;
-                spread = 0.0f;
+                spread = 0.0;
             }
             across += ri;
             spread += r2[n];
