@@ -52,11 +52,18 @@ __device__ __forceinline__ float exp_of(float v)
     return __builtin_fmaf(e, l * 0.693147181f, e);
 }
 
+// e^-|v|, no less than e^-100; not a number where v is none (a maximum would lose that).
+__device__ __forceinline__ float exp_down(float v)
+{
+    const float a = -fabsf(v);
+    return exp_of(a < -100.0f ? -100.0f : a);
+}
+
 // ln(1 + e^v) without overflow, and its derivative.  With e = e^-|v| and s = e / (2 + e) <= 1/3, ln(1 + e) = 2 artanh(s), of which
 // seven terms hold 2^-26; the hardware's logarithm loses digits where 1 + e is near 1.
 __device__ __forceinline__ float softplus(float v)
 {
-    const float e = exp_of(fmaxf(-fabsf(v), -100.0f)), d = 2.0f + e;
+    const float e = exp_down(v), d = 2.0f + e;
     const float r = __builtin_amdgcn_rcpf(d), q = e * r, s = __builtin_fmaf(__builtin_fmaf(-q, d, e), r, q), z = s * s;
     float p = __builtin_fmaf(z, 1.0f / 13.0f, 1.0f / 11.0f);
     p = __builtin_fmaf(p, z, 1.0f / 9.0f);
@@ -68,7 +75,7 @@ __device__ __forceinline__ float softplus(float v)
 }
 __device__ __forceinline__ float sigmoid(float v)
 {
-    const float e = exp_of(fmaxf(-fabsf(v), -100.0f));
+    const float e = exp_down(v);
     return (v < 0.0f ? e : 1.0f) / (1.0f + e);
 }
 
