@@ -65,8 +65,8 @@ template <class T> __global__ __launch_bounds__(256) void k_embed_fwd(EmbedArgs 
 __device__ __forceinline__ uint32_t key_of(const EmbedArgs &a, int i)
 {
     const int b = i / a.T, t = i % a.T;
-    const int32_t v = a.tokens[i];
-    return t < length_of(a.lengths, b, a.T) && v >= 0 && v < a.V ? (uint32_t)v : (uint32_t)a.V;
+    const int32_t v = t < length_of(a.lengths, b, a.T) ? a.tokens[i] : -1;
+    return v >= 0 && v < a.V ? (uint32_t)v : (uint32_t)a.V;
 }
 
 // The workgroups of a sorting launch beyond its tiles clear a share of the gradient.
@@ -276,9 +276,12 @@ template <class T, bool PAST> __global__ __launch_bounds__(256) void k_embed_sum
     const int id = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / 64), chunk = id / slices;
     const int col = (id % slices * 64 + lane) * E, first = chunk * a.chunk;
     if (chunk >= a.chunks) return;
-    const int n = first + a.chunk < a.n ? a.chunk : a.n - first;
-    const uint32_t mine = lane < n ? key[first + lane] : ~0u, at = lane < n ? pos[first + lane] : 0;
-    const uint32_t last = first + n < a.n ? key[first + n] : ~0u;  // the key behind the chunk
+    const int all = first + a.chunk < a.n ? a.chunk : a.n - first;
+    const uint32_t mine = lane < all ? key[first + lane] : ~0u, at = lane < all ? pos[first + lane] : 0;
+    // positions without a token are the last, and their rows are not read
+    const int n = __popcll(__ballot(mine < (uint32_t)a.V));
+    if (n == 0) return;
+    const uint32_t last = first + n < a.n ? key[first + n] : ~0u;  // the key behind them
     uint32_t run = first > 0 ? key[first - 1] : ~0u;
     const bool here = col < a.D;
     const T *g = (const T *)a.g + (here ? col : 0);
@@ -306,7 +309,6 @@ template <class T, bool PAST> __global__ __launch_bounds__(256) void k_embed_sum
             const int i = i0 + k;
             if (i >= n) break;
             const uint32_t v = (uint32_t)__builtin_amdgcn_readlane((int)mine, i);
-            if (v >= (uint32_t)a.V) return;  // positions without a token are the last
 #pragma unroll
             for (int e = 0; e < E; ++e) s[e] += (float)r[k][e];
             const bool ends = (i + 1 < n ? (uint32_t)__builtin_amdgcn_readlane((int)mine, i + 1) : last) != v;
