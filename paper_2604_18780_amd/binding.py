@@ -568,6 +568,13 @@ def _index(t, shape):
     return _plain(t, torch.int32, shape)
 
 
+def _bytes(t):
+    """Pointer and size of a workspace."""
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("expected a contiguous device tensor as workspace")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
 def _scratch(entry, sizes, device):
     """A workspace of the size the library asks for (torch aligns it to 512 bytes)."""
     n = ctypes.c_size_t(0)
@@ -596,7 +603,7 @@ def semicrf_embed_bwd(tokens, grad_out, V, scale=1.0, lengths=None, workspace=No
         grad_table = torch.empty((V, D), dtype=torch.float32, device=grad_out.device)
     _check(load().semicrf_embed_bwd(_index(tokens, (B, T)), _index(lengths, (B,)),
                                     _plain(grad_out, grad_out.dtype, (B, T, D)), scale, B, T, V, D, _act(grad_out),
-                                    workspace.data_ptr(), workspace.numel(), _plain(grad_table, torch.float32, (V, D)),
+                                    *_bytes(workspace), _plain(grad_table, torch.float32, (V, D)),
                                     _stream()))
     return grad_table
 
@@ -628,7 +635,7 @@ def semicrf_conv_bwd(u, weight, bias, grad_out, lengths=None, flags=0, workspace
     gb = torch.empty(C, dtype=torch.float32, device=dev)
     _check(load().semicrf_conv_bwd(*_rows(u, u.dtype, (B, T, C)), _param(weight, (C, W)), _param(bias, (C,)),
                                    _index(lengths, (B,)), *_rows(grad_out, u.dtype, (B, T, C)), B, T, C, W,
-                                   flags | _act(u), workspace.data_ptr(), workspace.numel(),
+                                   flags | _act(u), *_bytes(workspace),
                                    *_rows(grad_u, u.dtype, (B, T, C)), gw.data_ptr(), gb.data_ptr(), _stream()))
     return grad_u, gw, gb
 
@@ -654,7 +661,7 @@ def semicrf_ssm_fwd(x, b, c, dt, rate, skip=None, dt_bias=None, lengths=None, st
         out = torch.empty((B, T, H, P), dtype=x.dtype, device=x.device)
     if state_out is None and want_state:
         state_out = torch.empty((B, H, P, N), dtype=torch.float32, device=x.device)
-    _check(load().semicrf_ssm_fwd(*inputs, *sizes, _act(x), workspace.data_ptr(), workspace.numel(),
+    _check(load().semicrf_ssm_fwd(*inputs, *sizes, _act(x), *_bytes(workspace),
                                   *_rows(out, x.dtype, (B, T, H, P)), _param(state_out, (B, H, P, N)), _stream()))
     return out, state_out
 
@@ -676,7 +683,7 @@ def semicrf_ssm_bwd(x, b, c, dt, rate, skip, dt_bias, grad_y, lengths=None, stat
     heads = torch.empty((3, H), dtype=f32, device=dev)
     gstate = torch.empty((B, H, P, N), dtype=f32, device=dev) if want_state else None
     _check(load().semicrf_ssm_bwd(*inputs, *_rows(grad_y, dtype, (B, T, H, P)), _param(grad_state_out, (B, H, P, N)), *sizes,
-                                  _act(x), workspace.data_ptr(), workspace.numel(), *_rows(gx, dtype, (B, T, H, P)),
+                                  _act(x), *_bytes(workspace), *_rows(gx, dtype, (B, T, H, P)),
                                   *_rows(gb, dtype, (B, T, G, N)), *_rows(gc, dtype, (B, T, G, N)),
                                   *_rows(gdt, dtype, (B, T, H)), heads[0].data_ptr(), heads[1].data_ptr(),
                                   heads[2].data_ptr(), _param(gstate, (B, H, P, N)), _stream()))
