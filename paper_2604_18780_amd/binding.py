@@ -190,9 +190,15 @@ def _emis(t, flags):
     return _ptr(t, t.dtype), (flags & ~(SEMICRF_EMIS_F16 | SEMICRF_EMIS_BF16)) | bits[t.dtype]
 
 
+# Not part of torch's public interface, so a version of it may lack this.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream():
-    """The current HIP stream's handle (a tenth of what making a torch stream object for it costs)."""
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    """The current HIP stream's handle; the public way makes a stream object for it (2.7 us a call instead of 0.3)."""
+    if _raw_stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(torch.cuda.current_device())
 
 
 def alloc_workspace(B, T, K, C, ckpt_interval=0, want_grad=True, device="cuda:0"):
