@@ -73,7 +73,8 @@ class Encoder:
 
 
 class Stream:
-    """The encoder one token at a time, for `streams` texts side by side; `seen` < 0 marks one that is idle."""
+    """The encoder one token at a time, for `streams` texts side by side; `seen` < 0 marks one that is idle.  Its parameters are the
+    encoder's of when it was made, or of the last `refresh`: laid out once, not for every token."""
 
     def __init__(self, encoder, streams):
         self.enc = encoder
@@ -83,16 +84,23 @@ class Stream:
         self.seen = torch.zeros(streams, dtype=torch.int32, device=device)
         self.ring = torch.zeros(streams, *p["taps"].shape, dtype=encoder.dtype, device=device)
         self.state = torch.zeros(streams, H, P, N, device=device)
+        self.refresh()
+
+    def refresh(self):
+        """Takes the encoder's parameters as they are now; texts go on."""
+        p = self.enc.params
+        self.params = {k: p[k].to(self.enc.dtype, copy=True) for k in ("table", "w_in", "w_out")}
+        self.params.update({k: p[k].clone() for k in ("taps", "taps_bias", "skip", "dt_bias")}, rate=-torch.exp(p["log_rate"]))
 
     def step(self, tokens):
         """tokens [streams] int32 -> emission scores [streams,labels] of these positions."""
-        enc, p = self.enc, self.enc.params
+        enc, p = self.enc, self.params
         H, _, G, _ = enc.sizes
-        z = sb.semicrf_embed_fwd(tokens[:, None], p["table"].to(enc.dtype), enc.scale)[:, 0] @ p["w_in"].to(enc.dtype)
-        y = sb.semicrf_ssm_step(z[:, :enc.columns], p["taps"], p["taps_bias"], z[:, enc.columns:enc.columns + H],
-                                -torch.exp(p["log_rate"]), p["skip"], p["dt_bias"], self.seen, self.ring, self.state, groups=G)
+        z = sb.semicrf_embed_fwd(tokens[:, None], p["table"], enc.scale)[:, 0] @ p["w_in"]
+        y = sb.semicrf_ssm_step(z[:, :enc.columns], p["taps"], p["taps_bias"], z[:, enc.columns:enc.columns + H], p["rate"],
+                                p["skip"], p["dt_bias"], self.seen, self.ring, self.state, groups=G)
         self.seen += (self.seen >= 0).int()
-        return (y @ p["w_out"].to(enc.dtype)).float()
+        return (y @ p["w_out"]).float()
 
 
 def gold(labels, lengths, emis, crf):
