@@ -118,6 +118,20 @@ template <class T, int Q, int W, int NT, bool REV> struct Tile {
             }
         }
     }
+    // Sum of the products of this thread's elements of two operands.  (Not from the matrix cores: their sums are rounded one way, which
+    // shows in a sum over a million positions: 3e-5 of it.)
+    __device__ __forceinline__ float dot(const Tile &o) const
+    {
+        typedef T X __attribute__((ext_vector_type(E)));
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const X a = __builtin_bit_cast(X, r[i]), b = __builtin_bit_cast(X, o.r[i]);
+#pragma unroll
+            for (int e = 0; e < E; ++e) s = __builtin_fmaf((float)a[e], (float)b[e], s);
+        }
+        return s;
+    }
     // Where a lane reads.  Of a cell's number the mix changes its low four bits (three where a row is 32 wide), so the places of
     // all operands of a tile are four (two) numbers of the lane's and constants: the reads' own offsets.
     struct Lane {

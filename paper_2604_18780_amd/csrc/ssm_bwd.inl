@@ -127,7 +127,8 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
     __shared__ __attribute__((aligned(16))) __bf16 pool[2 * TP::ELEMS + 2 * TN::ELEMS + SC::ELEMS];
     __bf16 *const sx = pool, *const sy = sx + TP::ELEMS, *const sb = sy + TP::ELEMS, *const sc = sb + TN::ELEMS, *const sm = sc + TN::ELEMS;
     __shared__ Steps<Q> ss[2];  // of this head and the next
-    __shared__ float rp[NW][Q];             // by wave: its columns' part of rint
+    __shared__ float skips[HB][NT];         // by thread: sums for the skip, of at most 32 blocks
+    __shared__ __attribute__((aligned(16))) float rp[NW][Q];  // by wave: its columns' part of rint
     __shared__ float ends[SC::TILES][16];   // sums of a tile of W by its later positions (on the diagonal: dlin), ..
     __shared__ float starts[SC::TILES][16]; // .. and by its earlier ones
 
@@ -157,6 +158,7 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
         const int head = k < at.nh ? at.h0 + k : at.h0;
         rate[k] = a.rate[head];
         bias[k] = a.dt_bias ? a.dt_bias[head] : 0.0f;
+        skips[k][tid] = 0.0f;
         const float *from = a.hs + ((size_t)(at.b * a.H + head) * (a.nseg + 1) + at.seg) * cells;
 #pragma unroll
         for (int kt = 0; kt < KTP; ++kt) {
@@ -195,13 +197,14 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
         for (int it = 0; it < IT; ++it) O[it] = (f4)0.0f;
 #pragma unroll
         for (int k = 0; k < HB; ++k) {
-            if (k >= at.nh) break;
+            if (HB > 1 && k >= at.nh) break;
             rx.put(sx, plp, tid);
             ry.put(sy, plp, tid);
+            skips[k][tid] += rx.dot(ry);
             lds_barrier();
             // the next head's rows, or the next block's
             {
-                const bool last = k + 1 >= at.nh;
+                const bool last = HB == 1 || k + 1 >= at.nh;
                 if (last) src.move(Q);
                 const int left = last ? at.L - base - Q : at.L - base, col = last ? 0 : (k + 1) * a.P * E;
                 rx.fetch(rows_at(src.x, left, Q, src.x_bytes), col);
@@ -341,6 +344,20 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
 #pragma unroll
         for (int it = 0; it < IT; ++it) out.template put<Q>(base, i16, 16 * it, 16 * w + 4 * g, a.N, at.t1, O[it]);
     }
+    // sums for the skip: by wave in LDS, then over the waves in order
+    lds_barrier();
+#pragma unroll
+    for (int k = 0; k < HB; ++k) {
+        double s = skips[k][tid];
+        for (int d = 1; d < 64; d *= 2) s += __shfl_xor(s, d);
+        if (lane == 0) ((double *)rp[w])[k] = s;
+    }
+    lds_barrier();
+    if (tid < at.nh) {
+        double s = 0.0;
+        for (int y = 0; y < NW; ++y) s += ((const double *)rp[y])[tid];
+        a.skipp[(size_t)(at.b * a.H + at.h0 + tid) * a.nseg + at.seg] = s;
+    }
     if (a.chunks == 1)
         clear_rows<T>((T *)a.gc + at.rb * a.gc_row + at.grp * a.N, a.gc_row, at.t0 + at.nblk * Q, at.t1, a.N, tid, NT);
 }
@@ -394,14 +411,12 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
     f4 S[HB][KTN];               // G: rows n, this lane's column p
     f4 R[TWICE ? HB : 1][TWICE ? KTP : 1];  // its transpose: rows p, this lane's column n
     float rate[HB], bias[HB], skip[HB];
-    double skip_sum[HB];
 #pragma unroll
     for (int k = 0; k < HB; ++k) {
         const int head = k < at.nh ? at.h0 + k : at.h0;
         rate[k] = a.rate[head];
         bias[k] = a.dt_bias ? a.dt_bias[head] : 0.0f;
         skip[k] = a.skip ? a.skip[head] : 0.0f;
-        skip_sum[k] = 0.0;
         const float *from = a.gs + ((size_t)(at.b * a.H + head) * (a.nseg + 1) + at.seg + 1) * cells;
 #pragma unroll
         for (int kt = 0; kt < KTN; ++kt) {
@@ -526,12 +541,6 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
 #pragma unroll
                 for (int ks = 0; ks < KSP; ++ks)
                     p = mma_inputs(p, TP::by_row(sy, lp, jt, ks), TP::by_row(sx, lp, it, ks));
-                if (it == jt) {
-                    float on = 0.0f;  // the diagonal's
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) on += 4 * g + r == i16 ? p[r] : 0.0f;
-                    skip_sum[k] += (double)on;
-                }
 #pragma unroll
                 for (int o = 1; o < OWN; ++o)
                     if (o == own) d = D[o];
@@ -620,19 +629,6 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
     }
     lds_barrier();
     if (at.nblk) join(at.nblk - 1, at.nh - 1, true);
-    // sums for the skip: by wave in LDS, then over the waves in order
-    lds_barrier();
-#pragma unroll
-    for (int k = 0; k < HB; ++k) {
-        for (int d = 1; d < 64; d *= 2) skip_sum[k] += __shfl_xor(skip_sum[k], d);
-        if (lane == 0) ((double *)qp[0][w])[k] = skip_sum[k];
-    }
-    lds_barrier();
-    if (tid < at.nh) {
-        double s = 0.0;
-        for (int y = 0; y < NW; ++y) s += ((const double *)qp[0][y])[tid];
-        a.skipp[(size_t)(at.b * a.H + at.h0 + tid) * a.nseg + at.seg] = s;
-    }
     clear_rows<T>((T *)a.gx + at.rb * a.gx_row + at.h0 * a.P, a.gx_row, at.t0 + at.nblk * Q, at.t1, at.nh * a.P, tid, NT);
     if (a.chunks == 1)
         clear_rows<T>((T *)a.gb + at.rb * a.gb_row + at.grp * a.N, a.gb_row, at.t0 + at.nblk * Q, at.t1, a.N, tid, NT);
