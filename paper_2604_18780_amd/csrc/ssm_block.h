@@ -91,17 +91,20 @@ template <class T, int Q, int W, int NT, bool REV> struct Tile {
             }
         }
     };
-    __device__ __forceinline__ void put(__bf16 *tile, const Place &to, int tid) const
+    // TURN: odd columns negated
+    template <bool TURN = false> __device__ __forceinline__ void put(__bf16 *tile, const Place &to, int tid) const
     {
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             if (ALL % NT != 0 && tid + NT * i >= ALL) break;
+            u4 raw = r[i];
+            if constexpr (TURN) raw ^= E == 8 ? (u4)0x80000000u : (u4){0u, 0x80000000u, 0u, 0x80000000u};
             if constexpr (RAW == 1) {
-                *(u2 *)(tile + to.a[i]) = (u2){r[i][0], r[i][1]};
-                *(u2 *)(tile + to.b[i]) = (u2){r[i][2], r[i][3]};
+                *(u2 *)(tile + to.a[i]) = (u2){raw[0], raw[1]};
+                *(u2 *)(tile + to.b[i]) = (u2){raw[2], raw[3]};
             } else if constexpr (RAW == 2) {
                 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
-                const Op<2> o = split<2>(__builtin_convertvector(__builtin_bit_cast(h8, r[i]), f8));
+                const Op<2> o = split<2>(__builtin_convertvector(__builtin_bit_cast(h8, raw), f8));
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const u4 v = __builtin_bit_cast(u4, o.p[j]);
@@ -109,7 +112,7 @@ template <class T, int Q, int W, int NT, bool REV> struct Tile {
                     *(u2 *)(tile + to.b[i] + j * PART) = (u2){v[2], v[3]};
                 }
             } else {
-                const f4 v = __builtin_bit_cast(f4, r[i]);
+                const f4 v = __builtin_bit_cast(f4, raw);
                 float x[4] = {v[0], v[1], v[2], v[3]};
                 uint32_t p[3][2];
                 split_pairs<3, 2>(x, p);
@@ -118,8 +121,8 @@ template <class T, int Q, int W, int NT, bool REV> struct Tile {
             }
         }
     }
-    // Sum of the products of this thread's elements of two operands.  (Not from the matrix cores: their sums are rounded one way, which
-    // shows in a sum over a million positions: 3e-5 of it.)
+    // Sum of the products of this thread's elements of two operands, for sums over a text, which the matrix cores' rounding spoils
+    // (3e-5 of a sum over 800 000 positions in float32).
     __device__ __forceinline__ float dot(const Tile &o) const
     {
         typedef T X __attribute__((ext_vector_type(E)));

@@ -408,8 +408,8 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
     rbt.init(src.b_bytes, a.N, tid);
     rct.init(src.c_bytes, a.N, tid);
 
-    f4 S[HB][KTN];               // G: rows n, this lane's column p
-    f4 R[TWICE ? HB : 1][TWICE ? KTP : 1];  // its transpose: rows p, this lane's column n
+    f4 S[HB][KTN];               // G: rows n, this lane's column p (odd ones negated, here, in LDS and in U)
+    f4 R[TWICE ? HB : 1][TWICE ? KTP : 1];  // its transpose: rows p (odd ones negated), this lane's column n
     float rate[HB], bias[HB], skip[HB];
 #pragma unroll
     for (int k = 0; k < HB; ++k) {
@@ -422,11 +422,12 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
         for (int kt = 0; kt < KTN; ++kt) {
             const int row = 16 * kt + 4 * g;
             S[k][kt] = at.nblk && row < a.N && c0 < a.P ? *(const f4 *)(from + (size_t)c0 * a.N + row) : (f4)0.0f;
+            if (c0 & 1) S[k][kt] = -S[k][kt];
             if constexpr (TWICE) {
                 R[k][kt] = (f4)0.0f;
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    if (at.nblk && row + r < a.P && n0 < a.N) R[k][kt][r] = from[(size_t)(row + r) * a.N + n0];
+                    if (at.nblk && row + r < a.P && n0 < a.N) R[k][kt][r] = (r & 1 ? -1.0f : 1.0f) * from[(size_t)(row + r) * a.N + n0];
             }
         }
     }
@@ -475,8 +476,8 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
 #pragma unroll
         for (int k = 0; k < HB; ++k) {
             if (k >= at.nh) break;
-            rx.put(sx, plp, tid);
-            ry.put(sy, plp, tid);
+            rx.template put<true>(sx, plp, tid);
+            ry.template put<true>(sy, plp, tid);
             Op<HELD> st[KSN];
             {
 #pragma unroll
@@ -616,7 +617,7 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
                 const int r = 16 * it + i16;
 #pragma unroll
                 for (int ks = 0; ks <= it / 2; ++ks) U[it] = SC::product(U[it], vy[ks], su, it, ks, lane);
-                const f4 e = U[it] * xv[it], o = U[it] * s.delta[r] + yv[it] * skip[k];
+                const f4 e = U[it] * xv[it], o = (U[it] * s.delta[r] + yv[it] * skip[k]) * (f4){1.0f, -1.0f, 1.0f, -1.0f};
                 const float sum = sum_rows(e[0] + e[1] + e[2] + e[3]);
                 if (g == 0) xp[w][r] = sum;
                 store_four<T>(rows_at(gxs, at.t1 - base, Q, gx_bytes), gx_off, 16 * (IT - 1 - it) * gx_bytes + k * a.P * E, o);

@@ -120,7 +120,7 @@ __device__ __forceinline__ void scan_segment(const SsmArgs &a, unsigned block, S
         }
         if constexpr (OUT) rq.put(sq, pk, tid);
         rk.put(sk, pk, tid);
-        rv.put(sv, pv, tid);
+        rv.template put<!OUT>(sv, pv, tid);
         lds_barrier();
         if (n + 1 < nblk) fetch(n + 1);
         f4 O[IT];
@@ -201,7 +201,7 @@ __device__ __forceinline__ void scan_segment(const SsmArgs &a, unsigned block, S
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
             const int n = 16 * kt + 4 * g;
-            if (n < a.N && p < a.P) *(f4 *)(to + (size_t)p * a.N + n) = S[kt];
+            if (n < a.N && p < a.P) *(f4 *)(to + (size_t)p * a.N + n) = !OUT && (i16 & 1) ? -S[kt] : S[kt];
         }
     }
     if constexpr (OUT) {

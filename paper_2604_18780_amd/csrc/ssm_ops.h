@@ -3,6 +3,9 @@
 // The matrix cores multiply bfloat16.  Operands that are wider are split into bfloat16 parts whose sum holds 8, 16 or 24
 // bits, and the products of parts that matter are added up in 32 bits: bfloat16 inputs are exact in one part, float16 in two,
 // float32 takes three, and so does what is computed on the way (states, scores), whatever the type: 24 bits, 2^-25 of a term.
+// The matrix cores round their sums downwards, by some 2e-8 of a result; sums over a whole text of what has been multiplied by
+// values that are mostly positive collect that.  So what goes into such sums is computed with odd channels negated, from
+// their rows in LDS on: an error of either sign for every other channel, and nothing to pay but a sign.
 //
 // With g = lane / 16, a lane holds rows 4g..4g+3 of one column of a 16 x 16 result, and eight inner indexes of one row (or column)
 // of an operand: any eight, as long as both operands hold the same.  They are 4g..4g+3 of each of two tiles of 16, so that two
