@@ -8,7 +8,7 @@
 // of channels and walks a run of positions with the window in registers, the next four rows on their way while four are
 // worked on; sixteen threads side by side make 256-byte rows.
 // Measured, bfloat16, 4 x 100 000 positions of 640 channels, width 4: forwards 193 us (5.3 TB/s), backwards 371 us (4.1 TB/s; a sigmoid
-// and fifteen multiply-adds for each element keep the vector units half busy) and 15 us for the parameters' parts.
+// and fifteen multiply-adds for each element keep the vector units half busy, and 242 registers leave two waves a SIMD) and 15 us for the parameters' parts.
 #include "encoder.h"
 
 namespace semicrf_enc {

@@ -45,10 +45,10 @@ struct SsmArgs {
 };
 
 // Positions of a block of the gradient kernels.  Blocks of 64 read a state half as often, but want 250 registers, two waves to a SIMD,
-// where blocks of 32 run three: 4 x 100 000 tokens, 8 heads of 64, 64 states, bfloat16 took 611 + 1053 us with blocks of 64 and takes
-// 485 + 627 (16 x 4000 tokens, 32 heads of 16, 32 states 910 and 575).
+// where blocks of 32 run three: gradients of 4 x 100 000 tokens, 8 heads of 64, 64 states, bfloat16 2365 us with blocks of 64 and
+// 1713 with blocks of 32 (16 x 4000 tokens, 32 heads of 16, 32 states 765 and 568).
 // Heads that a workgroup of the gradient kernels takes where B and C are shared: one needs fewer registers, but leaves a part of the
-// gradients of B and C for each head (694 + 451 us and 331 to sum the parts, against 627 + 485 and 176), four spill.
+// gradients of B and C for each head (1814 us instead of 1713), four spill.
 constexpr int GRAD_BLOCK = 32, GRAD_HEADS = 2;
 
 // One instantiation per storage type, each in a translation unit of its own: outputs, or states alone (forwards, or both ways in

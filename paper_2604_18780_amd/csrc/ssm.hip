@@ -92,7 +92,7 @@ __global__ __launch_bounds__(64) void k_ssm_chain(SsmArgs a, bool grad)
 // walk, and all positions of a block share it.  What the walk is off by at the segment's start is therefore taken back: each value
 // by the share that its variance has of the difference's, both ends' included, with the squares of what has been added up
 // (all of it rounded alike) as variances.  Where a block keeps less than 2^-30, nothing is left of the difference but rounding:
-// `across` is 0, and the walk begins anew.  One wave per (sequence, head, segment); bound by latency, 60 to 80 us of the 2030 that
+// `across` is 0, and the walk begins anew.  One wave per (sequence, head, segment); bound by latency, 60 to 80 us of the 2110 that
 // training on 4 x 100 000 positions of 8 heads takes.
 constexpr int MOST_BLOCKS = 32;  // of a segment of 1024
 
@@ -360,7 +360,7 @@ struct SsmPlan {
 
 // Positions of a segment, by sequences and what a workgroup takes of each: as many segments as make three workgroups to a compute
 // unit, which is what the registers of most kernels let run at once; more would only add states to hand on (twice as many:
-// training on 32 x 1999 positions of 8 heads 407 us instead of 385, 400 000 positions of 8 heads forwards 450 instead of 444),
+// training on 32 x 1999 positions of 8 heads 438 us instead of 411, 400 000 positions of 8 heads forwards 493 instead of 465),
 // and shorter ones than 256 positions cost more than their share of the states.
 int segment_length(int B, int T, int H)
 {

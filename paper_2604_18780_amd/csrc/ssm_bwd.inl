@@ -12,9 +12,9 @@
 //   qint[j]  pairs that end behind j's block: u_j . (its gradient from the state)
 // k_ssm_steps joins them.
 //
-// Measured, bfloat16, 4 x 100 000 positions of 8 heads, 64 channels, 64 states: gradient of C 520 us, gradients of x and B 700 us.  Bound by
-// the instructions around the products: of the latter's time the vector units are busy 53 %, LDS 48 %, the matrix cores 21 %, at
-// three waves on a SIMD.
+// Measured, bfloat16, 4 x 100 000 positions of 8 heads, 64 channels, 64 states: gradient of C 569 us, gradients of x and B 716 us
+// under a trace.  Bound by the instructions around the products: of the latter's time the vector units are busy 49 %, LDS 45 %, the
+// matrix cores 21 %, at three waves on a SIMD.
 #ifndef SEMICRF_SSM_BWD_INL
 #define SEMICRF_SSM_BWD_INL
 
@@ -22,8 +22,8 @@
 
 namespace semicrf_enc {
 
-// Waves to a SIMD that the registers are cut for (16 x 4000 positions, 8 heads of 64, 64 states, float16: 475 us with two, 439 with
-// three; what is wider spills).
+// Waves to a SIMD that the registers are cut for (16 x 4000 positions, 8 heads of 64, 64 states, float16: 501 us with two, 452 with
+// three, though its gradients of x and B get two either way, for 70 KB of LDS; what is wider spills).
 constexpr int waves_for(int raw, int most) { return most <= 64 && raw <= 2 ? 3 : 2; }
 
 // What both kernels know of their workgroup.
@@ -390,8 +390,8 @@ template <class T, int PP, int NN, int HB> __global__ __launch_bounds__((PP > NN
     if (!at.any) return;
     const size_t cells = (size_t)a.P * a.N;
     // Where there are more waves than columns of P, some hold the same ones, and only the first of them write: without a branch the
-    // compiler finds the registers (8 x 4000 positions, 8 heads of 64, 128 states: bfloat16 390 us, 437 with one, 420 with P padded
-    // to 128 as well).  Columns of N are few enough to be branched on.
+    // compiler finds the registers (8 x 4000 positions, 8 heads of 64, 128 states: bfloat16 391 us, with one an eighth more, and with P
+    // padded to 128 as well a twelfth).  Columns of N are few enough to be branched on.
     const int wp = w % KTP, c0 = 16 * wp + i16, n0 = 16 * w + i16;  // this lane's columns
     const bool own_n = NN == MOST || 16 * w < NN;
 

@@ -10,9 +10,9 @@
 //   state   S[n,p] = e^{c_Q} S[n,p] + sum_j B[j,n] (e^{c_Q-c_j} delta_j x[j,p])
 // Steps (delta, c) are made for four blocks at a time, one by each wave.
 //
-// Measured, bfloat16, 400 000 positions of 8 heads, 64 channels, 64 states: outputs 296 us, 922 MB (3.1 TB/s); states alone 129 us, 461 MB
-// (3.6 TB/s).  Bound by no unit: of the outputs' time the vector units are busy 45 %, LDS 55 % and the matrix cores 29 %; what is
-// left is the latency from one to the next with three waves on a SIMD (155 registers).
+// Measured, bfloat16, 400 000 positions of 8 heads, 64 channels, 64 states: outputs 318 us, 922 MB (2.9 TB/s); states alone 125 us, 461 MB
+// (3.7 TB/s).  Bound by no unit: of the outputs' time the vector units are busy 48 %, LDS 50 % and the matrix cores 33 %; what is
+// left is the latency from one to the next with three waves on a SIMD (157 registers).
 #ifndef SEMICRF_SSM_FWD_INL
 #define SEMICRF_SSM_FWD_INL
 
@@ -36,8 +36,8 @@ __device__ __forceinline__ void scan_segment(const SsmArgs &a, unsigned block, S
     constexpr int NT = PV * 4, NW = PV / 16, KT = DK / 16, KS = DK / 32, IT = Q / 16, QS = Q / 32;
     constexpr int AHEAD = ScanShared<T, Q, DK, PV, OUT>::AHEAD;
     constexpr int RAW = Parts<T>::raw;
-    // queries are kept from the scores to the output, except where they would take 96 registers (float32, 128 states: 343 us so, 305
-    // read again; bfloat16 138 us kept, 154 read again; 16 x 4000 positions of 8 heads of 64)
+    // queries are kept from the scores to the output, except where they would take 96 registers (float32, 128 states: 488 us so, 303
+    // read again; bfloat16 144 us kept, 174 read again; 16 x 4000 positions of 8 heads of 64)
     constexpr bool HOLD = IT * KS * RAW <= 16;
     typedef Tile<T, Q, DK, NT, REV> TK;
     typedef Tile<T, Q, PV, NT, REV> TV;
@@ -238,8 +238,8 @@ template <class T, int Q, int DK, int PV> int launch_scan(bool out, bool both, c
 }
 // Positions of a block: 64 as long as the staged parts leave room for two workgroups on a compute unit, and the rows on their way
 // take few of a thread's registers (narrow heads have few threads for as many rows of B and C).  16 x 4000 positions of 512
-// channels, with blocks of 64 and of 32: float32, heads of 32, 32 states 243 and 172 us; float16, heads of 16, 64 states 532 and
-// 303; bfloat16, heads of 32, 128 states 250 and 182, heads of 16, 64 states 210 and 232.
+// channels, with blocks of 64 and of 32: float32, heads of 32, 32 states 238 and 165 us; float16, heads of 16, 64 states 588 and
+// 327; bfloat16, heads of 32, 128 states 246 and 181, heads of 16, 64 states 217 and 246.
 template <class T> constexpr int scan_block(int DK, int PV)
 {
     constexpr int R = Parts<T>::raw;
